@@ -294,6 +294,165 @@ int tsfm_gemm_bf16(void *stream, const void *A, const void *W, float *C,
 int tsfm_gemm_bf16_static(void *stream, const void *A, const void *W, float *C,
                           int32_t M, int32_t N, int32_t Kd);
 
+/* ---------------------------------------------------------------------------------------------
+ * Serving over a cache of pages.
+ *
+ * A decoder handle keeps one contiguous cache block of full capacity per series.  The calls below
+ * are the steps of a round for callers that manage the cache themselves, as a server of many
+ * series or of a model over quantised values (tokens) does: append the new tokens' keys and values
+ * with their rotary positions, attend the new tokens to the cache, verify drafted tokens, and, for
+ * streams that never end, evict what got little attention.  As in a decoder every cache position
+ * derives from the committed length len[b], which only tsfm_verify_tokens (and tsfm_cache_evict)
+ * moves: the round's tokens lie in slots len[b] .. len[b] + n_new[b] - 1, and what a verification
+ * rejects is garbage behind the new length.
+ *
+ * All four enqueue kernels on `stream` and return; they allocate nothing, keep nothing between
+ * calls, and can be captured into a CUDA graph.  Pointers are dev on the current device unless
+ * said otherwise; `stream` belongs to the current device.  Two calls that overlap on the GPU must
+ * not share a workspace, nor pages that one of them writes.
+ *
+ * A pool holds pages of page_size slots for all series.  Slot s of series b lies in page
+ * table[b * table_stride + s / page_size]; element i of its key for head h is
+ *     k[page * page_stride + h * head_stride + (s % page_size) * slot_stride + i]
+ * (strides in elements), its value likewise in v.  Page ids are read up to the series' length
+ * only.  Device data that is wrong does not fault: an id outside [0, n_pages) is never
+ * followed (its slots are hidden from attention, appends to it are dropped, an eviction copies
+ * nothing from or to it) and sets TSFM_PAGES_BAD_ID in *status; a length below 0 or beyond the
+ * capacity is cut to it and sets TSFM_PAGES_BAD_LEN.  *status is only ever OR-ed into.
+ *
+ * Restrictions (TSFM_ERR_SHAPE): d_head 32, 64 or 128; page_size a power of two up to 65536;
+ * pointers to keys, values, queries and outputs and their strides multiples of 16 bytes. */
+#define TSFM_PAGES_BAD_ID  1
+#define TSFM_PAGES_BAD_LEN 2
+
+typedef struct {
+  void          *k, *v;         /* dev pools of `dtype`                                         */
+  int64_t        page_stride, head_stride, slot_stride;
+  const int32_t *table;         /* dev [B, table_stride]; pages of a series in slot order       */
+  int32_t        table_stride;
+  int32_t        max_pages;     /* entries of a row that may be used: capacity max_pages * page_size */
+  int32_t        n_pages;       /* pages in the pool                                            */
+  int32_t        page_size;
+  int32_t        n_kv_heads, d_head;
+  int32_t        dtype;         /* TSFM_F32 | TSFM_BF16, of the cache, the queries and the outputs */
+  int32_t       *status;        /* dev, nullable                                                */
+} tsfm_kv_pages;
+
+/* Rotary positions.  The leading rot_dim elements of a head turn in pairs: pair i < rot_dim / 2 at
+ * position t goes (x, y) -> mscale (x cos a - y sin a, x sin a + y cos a), a = t f_i; the other
+ * elements stay.  HALF pairs elements i and i + rot_dim / 2 (the decoder's own layout), INTERLEAVED
+ * elements 2 i and 2 i + 1.  Frequencies, for base b and factor F:
+ *     PLAIN   f_i = b^(-2 i / rot_dim)
+ *     LINEAR  f_i / F                                  (positions divided by F)
+ *     BASE    PLAIN with b F^(rot_dim / (rot_dim - 2)) for b
+ *     PARTS   f_i (g_i + (1 - g_i) / F), g_i = clamp((n_i - turns_lo) / (turns_hi - turns_lo), 0, 1),
+ *             n_i = original_len f_i / (2 pi): frequencies that turn often within the original
+ *             context stay, those that turn seldom are divided by F.
+ * mscale multiplies the turned elements (1 for none). */
+#define TSFM_ROPE_HALF        0
+#define TSFM_ROPE_INTERLEAVED 1
+#define TSFM_ROPE_PLAIN  0
+#define TSFM_ROPE_LINEAR 1
+#define TSFM_ROPE_BASE   2
+#define TSFM_ROPE_PARTS  3
+typedef struct {
+  int32_t  layout, rot_dim;
+  float    mscale;
+  int32_t  reserved0;
+  uint64_t turn[64];            /* 2^64 x turns of pair i per position, modulo 2^64               */
+} tsfm_rope;
+
+/* Fill *rope (host; host arithmetic only).  TSFM_ERR_ARG: rope NULL, unknown layout or scaling,
+ * rot_dim odd, negative or above 128, base or factor not finite or < 1 (base > 1), mscale not finite,
+ * BASE with rot_dim 2, PARTS without original_len > 0 and 0 <= turns_lo < turns_hi.  The last
+ * three numbers count for PARTS only. */
+int tsfm_rope_init(tsfm_rope *rope, int32_t layout, int32_t rot_dim, int32_t scaling, double base, double factor,
+                   double original_len, double turns_lo, double turns_hi, float mscale);
+
+/* Turn the queries and keys of up to M new tokens per series and append keys and values to the
+ * cache.  Token m < n_new[b] of series b has position pos[b] + m and slot len[b] + m.
+ *   qkv     [B, M] rows of (n_heads + 2 n_kv_heads) * d_head elements, qkv_stride elements apart: the
+ *           query heads, the key heads, the value heads (one product with stacked weights)
+ *   q_out   [B, M] rows of n_heads * d_head, q_out_stride apart: turned queries.  May be qkv itself
+ *           (same stride: in place), otherwise disjoint from it; NULL: queries are not touched
+ *   pos     [B] position of the first new token; NULL: len (they part once slots are evicted)
+ *   len     [B] slots already in the cache
+ *   n_new   [B] new tokens, cut to 0 .. M; NULL: M each.  Rows behind them are not touched
+ * rope->rot_dim <= d_head; n_heads >= 0.  Pages that are written belong to one series only. */
+int tsfm_rope_append(void *stream, const tsfm_rope *rope, const tsfm_kv_pages *pages, const void *qkv, int64_t qkv_stride,
+                     void *q_out, int64_t q_out_stride, const int32_t *pos, const int32_t *len, const int32_t *n_new,
+                     int32_t B, int32_t M, int32_t n_heads);
+
+/* Attention of up to M new tokens per series over the cache.  Token m < n_new[b], head h, reads key
+ * head h / (n_heads / n_kv_heads); it sees slots max(0, end - window) <= s < end, where end is
+ * len[b] + m + 1 with `causal` (the new tokens are in the cache, each sees those before it and
+ * itself) and len[b] without (they are not; encoder caches).  window 0: no lower bound.
+ *   out  softmax(scale q.k) v in fp32, rounded once;  lse  log of the sum of exp(scale q.k).
+ * A token that sees nothing (or only scores of -inf) gets out 0, lse -inf.  What lies in slots that a
+ * token does not see has no influence, NaN included.
+ *   q, out  [B, M] rows of n_heads * d_head, q_stride / out_stride elements apart
+ *   lse     [B, M, n_heads] fp32, nullable
+ *   w_out   nullable, [B, n_kv_heads] rows of w_stride fp32: w_out = w_in + the probabilities that a
+ *           slot got, summed over the series' new tokens and the heads of the group, for every slot
+ *           below len[b] + n_new[b] (len[b] without causal); behind them nothing is written.  w_in NULL
+ *           counts as 0 and may be w_out.  A series with n_new[b] <= 0 copies w_in.
+ *   max_len the longest series of the call in slots, new tokens included: lengths are cut to it.
+ *           It sizes the grid and the workspace, not the work.  w_stride >= max_len
+ *   workspace  256-byte aligned, tsfm_paged_attention_workspace() bytes; contents do not matter
+ * Rows of tokens m >= n_new[b] are not touched.  Results do not depend on the other series' lengths
+ * beyond rounding, and are the same each time for the same call. */
+int tsfm_paged_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                         const int32_t *len, const int32_t *n_new, int32_t B, int32_t M, int32_t n_heads, float scale,
+                         int32_t causal, int32_t window, int32_t max_len, float *lse, const float *w_in, float *w_out,
+                         int64_t w_stride, void *workspace, size_t workspace_bytes);
+
+/* Bytes of workspace for a call of this shape (host arithmetic only; of `pages` the shapes and the dtype
+ * count).  0 on invalid arguments. */
+size_t tsfm_paged_attention_workspace(const tsfm_kv_pages *pages, int32_t B, int32_t M, int32_t n_heads, int32_t max_len,
+                                      int32_t with_weights);
+
+/* Eviction by accumulated weight: per series and key head, the slots to keep become slots 0, 1, .. (in
+ * their old order) of the pages that dst_table names, in the same pool.  A series of L = len[b] <=
+ * budget slots keeps them all; otherwise the first `sinks`, the last `recent`, and of the slots between
+ * them the budget - sinks - recent with the largest w (equal ones: the lower slot; NaN counts as
+ * lowest).  Heads keep different slots; keys are stored turned, so attention does not ask where they
+ * were.  The old pages are not written: they may be shared, and are the caller's to release.
+ *   dst_table [B] rows of dst_stride page ids, at least ceil(budget / page_size) of them readable (up to
+ *             the kept slots' last); its pages belong to one series and to no row of pages->table
+ *   w         [B, n_kv_heads] rows of w_stride fp32 (as tsfm_paged_attention accumulates them)
+ *   max_len   the longest series in slots: lengths are cut to it.  w_stride >= max_len
+ *   kept      [B, n_kv_heads, budget] int32 out: old slot of each new one, ascending, -1 behind them
+ *   w_out     [B, n_kv_heads] rows of w_out_stride >= budget fp32, nullable: w of the kept slots; not
+ *             written behind them.  Must not overlap w
+ *   len_out   [B] out: min(L, budget); must not be len
+ * budget >= 1, sinks and recent >= 0, sinks + recent <= budget. */
+int tsfm_cache_evict(void *stream, const tsfm_kv_pages *pages, const int32_t *dst_table, int32_t dst_stride, const int32_t *len,
+                     const float *w, int64_t w_stride, int32_t B, int32_t budget, int32_t sinks, int32_t recent, int32_t max_len,
+                     int32_t *kept, float *w_out, int64_t w_out_stride, int32_t *len_out);
+
+/* Verification of drafted tokens: tsfm_accept_round's counterpart for heads that give a distribution
+ * over V tokens.  Proposals x_1..x_nd of series b (nd = n_draft[b], or K) are accepted from the left
+ * while u_i q_i(x_i) < p_i(x_i), compared exactly; after n acceptances the committed tokens are
+ * x_1..x_n and one drawn from r = max(p_{n+1} - q_{n+1}, 0) (n < nd: the first rejection) or r = p_{n+1}
+ * (n = nd: the bonus): the smallest t with r_0 + .. + r_t > u_{K+1} (r_0 + .. + r_{V-1}), in fp64.  Where r is 0
+ * everywhere r = p_{n+1}.  Entries of p and q that are negative or not finite count as 0, uniforms are
+ * cut to [0, 1 - 2^-24], a proposal outside [0, V) is rejected.
+ *   tokens  [B, K] int32 proposals
+ *   p       [B, K+1] rows of V fp32, p_stride elements apart: the target's probabilities at the boundaries
+ *   q       [B, K] rows of V fp32, q_stride apart: the draft's; NULL: proposals without a distribution
+ *           (the draft's best token), q_i is 1 at x_i and 0 elsewhere
+ *   u       [B, K+1] fp32 uniforms, the last one for the draw; NULL: the Philox uniforms of
+ *           tsfm_accept_round, counter (series0 + b, round_idx, position, 0), key = seed
+ *   n_draft [B], nullable, cut to 0 .. K; the draw of a series with fewer uses u_{K+1} all the same
+ *   out     [B, K+1] int32: the n + 1 committed tokens, -1 behind them (the drawn one is -1 too where p
+ *           has no positive entry)
+ *   n_accept [B] int32 out
+ *   len, len_out  [B] int32, both or neither: len_out = len + n + 1, the committed length; may be the same
+ * K <= TSFM_MAX_K; K = 0 draws one token.  out overlaps no input. */
+int tsfm_verify_tokens(void *stream, const int32_t *tokens, const float *p, int64_t p_stride, const float *q, int64_t q_stride,
+                       int32_t B, int32_t K, int32_t V, const float *u, uint64_t seed, int32_t round_idx, int32_t series0,
+                       const int32_t *n_draft, const int32_t *len, int32_t *out, int32_t *n_accept, int32_t *len_out);
+
 /* Bounds-checking mode only (TSFM_EXEC_CHECK_BOUNDS): *n_regions (nullable) receives the number of
  * guard regions of the handle.  region >= 0 additionally overwrites (damage != 0) or restores
  * (damage == 0) one byte of that guard region -- a write inside the library's own allocation --

@@ -21,11 +21,15 @@ TSFM_DRAFT_SEPARATE, TSFM_DRAFT_LAYER_SKIP = 0, 1
 TSFM_GEMM_AUTO, TSFM_GEMM_SIMT, TSFM_GEMM_WS = 0, 1, 2
 TSFM_EXEC_GRAPH, TSFM_EXEC_STREAM, TSFM_EXEC_NO_PDL, TSFM_EXEC_NO_COMPACT, TSFM_EXEC_CHECK_BOUNDS = 0, 1, 2, 4, 8
 TSFM_MAX_K = 32
+TSFM_PAGES_BAD_ID, TSFM_PAGES_BAD_LEN = 1, 2
+TSFM_ROPE_HALF, TSFM_ROPE_INTERLEAVED = 0, 1
+TSFM_ROPE_PLAIN, TSFM_ROPE_LINEAR, TSFM_ROPE_BASE, TSFM_ROPE_PARTS = 0, 1, 2, 3
 
 EXPORTS = [
     "tsfm_weights_bytes", "tsfm_weights_offset", "tsfm_weights_bytes_io", "tsfm_weights_offset_io", "tsfm_spec_create", "tsfm_spec_forecast", "tsfm_spec_forecast_variant",
     "tsfm_target_only_forecast", "tsfm_draft_only_forecast", "tsfm_spec_forecast_host", "tsfm_target_only_forecast_host",
     "tsfm_spec_last_trace", "tsfm_accept_round", "tsfm_model_forward", "tsfm_gemm_bf16", "tsfm_gemm_bf16_static",
+    "tsfm_rope_init", "tsfm_rope_append", "tsfm_paged_attention", "tsfm_paged_attention_workspace", "tsfm_cache_evict", "tsfm_verify_tokens",
     "tsfm_spec_debug_guard", "tsfm_spec_set_profiling", "tsfm_spec_kernel_profile", "tsfm_advise_block_size", "tsfm_spec_destroy", "tsfm_launch_count", "tsfm_strerror", "tsfm_last_cuda_error",
 ]
 
@@ -75,6 +79,19 @@ class tsfm_kernel_stat(C.Structure):
                 ("bytes", C.c_double), ("flops", C.c_double)]
 
 
+class tsfm_kv_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("slot_stride", C.c_int64),
+                ("table", C.c_void_p), ("table_stride", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int32),
+                ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32), ("dtype", C.c_int32),
+                ("status", C.c_void_p)]
+
+
+class tsfm_rope(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("rot_dim", C.c_int32), ("mscale", C.c_float), ("reserved0", C.c_int32),
+                ("turn", C.c_uint64 * 64)]
+
+
 def _load() -> C.CDLL:
     path = _build.LIB
     if not os.path.exists(path):
@@ -113,6 +130,19 @@ def _load() -> C.CDLL:
     lib.tsfm_gemm_bf16.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32]
     lib.tsfm_gemm_bf16_static.restype = C.c_int
     lib.tsfm_gemm_bf16_static.argtypes = [vp, vp, vp, vp, i32, i32, i32]
+    i64, f64, pages = C.c_int64, C.c_double, C.POINTER(tsfm_kv_pages)
+    lib.tsfm_rope_init.restype = C.c_int
+    lib.tsfm_rope_init.argtypes = [C.POINTER(tsfm_rope), i32, i32, i32, f64, f64, f64, f64, f64, f32]
+    lib.tsfm_rope_append.restype = C.c_int
+    lib.tsfm_rope_append.argtypes = [vp, C.POINTER(tsfm_rope), pages, vp, i64, vp, i64, vp, vp, vp, i32, i32, i32]
+    lib.tsfm_paged_attention.restype = C.c_int
+    lib.tsfm_paged_attention.argtypes = [vp, pages, vp, i64, vp, i64, vp, vp, i32, i32, i32, f32, i32, i32, i32, vp, vp, vp, i64, vp, sz]
+    lib.tsfm_paged_attention_workspace.restype = sz
+    lib.tsfm_paged_attention_workspace.argtypes = [pages, i32, i32, i32, i32, i32]
+    lib.tsfm_cache_evict.restype = C.c_int
+    lib.tsfm_cache_evict.argtypes = [vp, pages, vp, i32, vp, vp, i64, i32, i32, i32, i32, i32, vp, vp, i64, vp]
+    lib.tsfm_verify_tokens.restype = C.c_int
+    lib.tsfm_verify_tokens.argtypes = [vp, vp, vp, i64, vp, i64, i32, i32, i32, vp, u64, i32, i32, vp, vp, vp, vp, vp]
     lib.tsfm_spec_debug_guard.restype = C.c_int
     lib.tsfm_spec_debug_guard.argtypes = [vp, i32, i32, C.POINTER(i32)]
     lib.tsfm_spec_set_profiling.restype = C.c_int
@@ -299,6 +329,60 @@ def tsfm_gemm_bf16_static(stream, A, W, Cout, M: int, N: int, Kd: int) -> None:
     if code == TSFM_ERR_SHAPE:
         raise TsfmError(code, "tsfm_gemm_bf16_static: " + lib.tsfm_last_cuda_error().decode())
     _check(code, "tsfm_gemm_bf16_static")
+
+
+# ---------------------------------------------------------------- serving over a cache of pages
+def kv_pages(k, v, table, status=None) -> tsfm_kv_pages:
+    """Describe a pool: k, v [n_pages, n_kv_heads, page_size, d_head] tensors of one dtype and the same strides (a pool laid out
+    [n_pages, page_size, n_kv_heads, d_head] goes in as k.transpose(1, 2)), table [B, max_pages] int32.  The tensors stay the
+    caller's; the description holds their addresses."""
+    import torch
+    code = {torch.float32: TSFM_F32, torch.bfloat16: TSFM_BF16}.get(k.dtype)
+    if (code is None or v.dtype != k.dtype or k.dim() != 4 or v.shape != k.shape or v.stride() != k.stride() or k.stride(3) != 1
+            or table.dim() != 2 or table.dtype != torch.int32 or table.stride(1) != 1 or len({k.device, v.device, table.device}) != 1
+            or (status is not None and (status.dtype != torch.int32 or status.device != k.device))):
+        raise TsfmError(TSFM_ERR_ARG, "kv_pages")
+    return tsfm_kv_pages(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), table.data_ptr(), table.stride(0),
+                         table.shape[1], k.shape[0], k.shape[2], k.shape[1], k.shape[3], code, _ptr(status))
+
+
+def tsfm_rope_init(layout: int, rot_dim: int, scaling: int, base: float, factor: float = 1.0, original_len: float = 0.0,
+                   turns_lo: float = 0.0, turns_hi: float = 0.0, mscale: float = 1.0) -> tsfm_rope:
+    r = tsfm_rope()
+    _check(lib.tsfm_rope_init(C.byref(r), layout, rot_dim, scaling, base, factor, original_len, turns_lo, turns_hi, mscale),
+           "tsfm_rope_init")
+    return r
+
+
+def tsfm_rope_append(stream, rope: tsfm_rope, pages: tsfm_kv_pages, qkv, qkv_stride: int, q_out, q_out_stride: int, pos, len, n_new,
+                     B: int, M: int, n_heads: int) -> None:
+    _check(lib.tsfm_rope_append(stream, rope, pages, _ptr(qkv), qkv_stride, _ptr(q_out), q_out_stride, _ptr(pos), _ptr(len),
+                                _ptr(n_new), B, M, n_heads), "tsfm_rope_append")
+
+
+def tsfm_paged_attention_workspace(pages: tsfm_kv_pages, B: int, M: int, n_heads: int, max_len: int, with_weights: bool = False) -> int:
+    return int(lib.tsfm_paged_attention_workspace(pages, B, M, n_heads, max_len, int(bool(with_weights))))
+
+
+def tsfm_paged_attention(stream, pages: tsfm_kv_pages, q, q_stride: int, out, out_stride: int, len, n_new, B: int, M: int, n_heads: int,
+                         scale: float, causal: bool, window: int, max_len: int, lse, w_in, w_out, w_stride: int, workspace,
+                         workspace_bytes: int) -> None:
+    _check(lib.tsfm_paged_attention(stream, pages, _ptr(q), q_stride, _ptr(out), out_stride, _ptr(len), _ptr(n_new), B, M, n_heads,
+                                    scale, causal, window, max_len, _ptr(lse), _ptr(w_in), _ptr(w_out), w_stride, _ptr(workspace),
+                                    workspace_bytes), "tsfm_paged_attention")
+
+
+def tsfm_cache_evict(stream, pages: tsfm_kv_pages, dst_table, dst_stride: int, len, w, w_stride: int, B: int, budget: int, sinks: int,
+                     recent: int, max_len: int, kept, w_out, w_out_stride: int, len_out) -> None:
+    _check(lib.tsfm_cache_evict(stream, pages, _ptr(dst_table), dst_stride, _ptr(len), _ptr(w), w_stride, B, budget, sinks, recent,
+                                max_len, _ptr(kept), _ptr(w_out), w_out_stride, _ptr(len_out)), "tsfm_cache_evict")
+
+
+def tsfm_verify_tokens(stream, tokens, p, p_stride: int, q, q_stride: int, B: int, K: int, V: int, u, seed: int, round_idx: int,
+                       series0: int, n_draft, len, out, n_accept, len_out) -> None:
+    _check(lib.tsfm_verify_tokens(stream, _ptr(tokens), _ptr(p), p_stride, _ptr(q), q_stride, B, K, V, _ptr(u), seed, round_idx,
+                                  series0, _ptr(n_draft), _ptr(len), _ptr(out), _ptr(n_accept), _ptr(len_out)),
+           "tsfm_verify_tokens")
 
 
 def tsfm_spec_debug_guard(h, region: int = -1, damage: bool = False) -> int:

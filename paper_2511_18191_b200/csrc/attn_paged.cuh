@@ -1,0 +1,343 @@
+// Attention of a series' new tokens over its cache of pages (tsfm_paged_attention).
+//
+// Work: a unit is one series, one key head and up to ROWS of its query rows (new tokens x heads of the group: they read the
+// same keys).  A unit's slots are cut into tiles, the tiles of all units are numbered through, and every CTA takes an
+// equal run of them: lengths may differ by any factor and nothing waits for the longest series.  A run covers at most
+// two units in part, its first and its last; those leave (max, sum, unnormalised output) in the workspace, and
+// paged_join_kernel joins the parts in order.  Running maximum and sum per row, scores in base 2.
+#pragma once
+#include "pages.cuh"
+
+namespace tsfm {
+
+constexpr int PA_TILE = 64;                        // slots
+constexpr int PA_THREADS = 128;
+constexpr int PA_JOIN_WARPS = 4;
+
+// What a CTA that starts inside a unit leaves for the join: the unit, and the CTAs that share it.
+struct PagedMeta {
+  int b, u, c0, c1;                                // b < 0: nothing
+};
+
+struct PagedAttnArgs {
+  PagesDev pg;                                     // capacity: also cut to max_len
+  const void *q;
+  void *out;
+  long long q_stride, out_stride;                  // elements
+  const int *len, *n_new;                          // n_new or NULL
+  int B, M, n_heads, group;                        // group = n_heads / n_kv_heads
+  float scale2;                                    // scale * log2(e)
+  int causal, window;
+  float *lse;                                      // or NULL
+  const float *w_in;                               // or NULL
+  float *w_out;                                    // or NULL
+  long long w_stride;
+  int chunks, units;                               // row chunks of a key head, units of a series
+  PagedMeta *meta;                                 // [grid]
+  float2 *part_ml;                                 // [2 grid][rows]
+  float *part_o;                                   // [2 grid][rows][D]
+  float *lse2;                                     // [B][heads of keys][M group], with weights only
+  float *scores;                                   // [B][heads of keys][M group][score_stride], with weights only
+  long long score_stride;
+};
+
+// A series as this call sees it: its live rows, the slots that any of them sees, the tiles that hold those.
+struct PagedSpan {
+  int len, n_new, total, lo, tile0, tiles;
+};
+__device__ __forceinline__ PagedSpan paged_span(const PagedAttnArgs &a, int b, bool report) {
+  PagedSpan s;
+  const int raw = __ldg(a.len + b);
+  s.len = cut(raw, a.pg.capacity);
+  s.n_new = a.n_new ? cut(__ldg(a.n_new + b), a.M) : a.M;
+  const long long total = (long long)s.len + (a.causal ? s.n_new : 0);
+  s.total = (int)min(total, (long long)a.pg.capacity);
+  if (report && (raw != s.len || total != s.total)) pages_report(a.pg, BAD_LEN);
+  const int first_end = a.causal ? min(s.len + 1, s.total) : s.total;
+  s.lo = a.window ? max(0, first_end - a.window) : 0;
+  s.tile0 = s.lo / PA_TILE;
+  // a live row without slots still has an answer: one tile
+  s.tiles = s.n_new == 0 ? 0 : max(1, (s.total + PA_TILE - 1) / PA_TILE - s.tile0);
+  return s;
+}
+// Slots [lo, end) that row m sees.
+__device__ __forceinline__ int2 paged_row_range(const PagedAttnArgs &a, const PagedSpan &s, int m) {
+  const int end = m >= s.n_new ? 0 : a.causal ? min(s.len + m + 1, s.total) : s.total;
+  return make_int2(a.window ? max(0, end - a.window) : 0, end);
+}
+
+// The CTA's run of tiles: `count` of them from tile `first` of unit `u` of series `b`; per: tiles a CTA; unit0: number of that
+// unit's first tile.
+struct PagedRun {
+  int b, u, first, count;
+  long long unit0, per;
+};
+// Every thread sums the tiles of a contiguous share of the series, a block scan places them.
+template <int THREADS>
+__device__ PagedRun paged_find_run(const PagedAttnArgs &a) {
+  __shared__ long long warp_sum_s[THREADS / 32];
+  __shared__ PagedRun found;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int share = (a.B + THREADS - 1) / THREADS, b0 = min(a.B, tid * share), b1 = min(a.B, b0 + share);
+  long long mine = 0;
+  for (int b = b0; b < b1; ++b) mine += (long long)paged_span(a, b, blockIdx.x == 0).tiles * a.units;
+  long long inc = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += v;
+  }
+  if (lane == 31) warp_sum_s[warp] = inc;
+  if (tid == 0) found.b = -1, found.count = 0;
+  __syncthreads();
+  long long before = inc - mine, total = 0;
+  for (int i = 0; i < THREADS / 32; ++i) {
+    if (i < warp) before += warp_sum_s[i];
+    total += warp_sum_s[i];
+  }
+  const long long per = max(1ll, (total + gridDim.x - 1) / gridDim.x), start = per * blockIdx.x;
+  if (start >= before && start < before + mine) {
+    for (int b = b0; b < b1; ++b) {
+      const int tiles = paged_span(a, b, false).tiles;
+      const long long here = (long long)tiles * a.units;
+      if (start < before + here) {
+        const int u = (int)((start - before) / tiles), first = (int)((start - before) - (long long)u * tiles);
+        found = PagedRun{b, u, first, (int)min(per, total - start), start - first, per};
+        break;
+      }
+      before += here;
+    }
+  }
+  __syncthreads();
+  return found;
+}
+
+// Where a row's result goes: straight to the caller, or as a part into the workspace.
+__device__ __forceinline__ void paged_write_lse(const PagedAttnArgs &a, int b, int h, int row, float m, float l) {
+  const int tok = row / a.group, head = h * a.group + row - tok * a.group;
+  const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
+  if (a.lse) a.lse[((long long)b * a.M + tok) * a.n_heads + head] = lse2 * 0.69314718055994530942f;
+  if (a.lse2) a.lse2[((long long)b * a.pg.n_kv_heads + h) * a.M * a.group + row] = lse2;
+}
+template <typename T>
+__device__ __forceinline__ T *paged_out_row(const PagedAttnArgs &a, int b, int h, int row, int D) {
+  const int tok = row / a.group, head = h * a.group + row - tok * a.group;
+  return reinterpret_cast<T *>(a.out) + ((long long)b * a.M + tok) * a.out_stride + (long long)head * D;
+}
+
+// The FMA kernel.  Eight lanes share a slot, a warp works on four at a time, each group of eight lanes with its own running
+// maximum and sum; nothing is staged.
+template <typename T, int D, int ROWS>
+__global__ void __launch_bounds__(PA_THREADS) paged_attn_fma_kernel(const __grid_constant__ PagedAttnArgs a) {
+  constexpr int E = D / 8, V = Pack16<T>::N < E ? Pack16<T>::N : E, NV = E / V;       // elements a lane, of a load, loads
+  constexpr int WARPS = PA_THREADS / 32, KEYS = 2;                                  // slots of a group in flight
+  __shared__ float s_o[WARPS][ROWS][D];
+  __shared__ float2 s_ml[WARPS][ROWS];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l8 = lane & 7, grp = lane >> 3;
+  PagedRun run = paged_find_run<PA_THREADS>(a);
+  if (threadIdx.x == 0) {
+    PagedMeta meta{-1, 0, 0, 0};
+    if (run.count > 0 && run.first) {
+      const int tiles = paged_span(a, run.b, false).tiles;
+      meta = PagedMeta{run.b, run.u, (int)(run.unit0 / run.per), (int)((run.unit0 + tiles - 1) / run.per)};
+    }
+    a.meta[blockIdx.x] = meta;
+  }
+  while (run.count > 0) {
+    const PagedSpan s = paged_span(a, run.b, false);
+    if (s.tiles == 0) {                                          // (a finished series: no units)
+      ++run.b, run.u = 0;
+      continue;
+    }
+    const int take = min(run.count, s.tiles - run.first);
+    const int h = run.u / a.chunks, row0 = (run.u - h * a.chunks) * ROWS, rows = min(ROWS, a.M * a.group - row0);
+    const int *table = a.pg.table + (long long)run.b * a.pg.table_stride;
+    float q[ROWS][E], o[ROWS][E], m[ROWS], l[ROWS];
+    int2 range[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      m[r] = -INFINITY;
+      l[r] = 0.f;
+      range[r] = r < rows ? paged_row_range(a, s, (row0 + r) / a.group) : make_int2(0, 0);
+      const int tok = r < rows ? (row0 + r) / a.group : 0, head = h * a.group + (r < rows ? row0 + r - tok * a.group : 0);
+      const T *src = reinterpret_cast<const T *>(a.q) + ((long long)run.b * a.M + tok) * a.q_stride + (long long)head * D;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        o[r][e] = 0.f;
+        q[r][e] = to_f32(src[e / V * 8 * V + l8 * V + e % V]);
+      }
+    }
+    for (int t = run.first; t < run.first + take; ++t) {
+      const int base = (s.tile0 + t) * PA_TILE + warp * (PA_TILE / WARPS);
+#pragma unroll 1
+      for (int i = 0; i < PA_TILE / WARPS; i += 4 * KEYS) {
+        T kx[KEYS][E], vx[KEYS][E];
+        bool live[KEYS];
+#pragma unroll
+        for (int j = 0; j < KEYS; ++j) {
+          const int slot = base + i + 4 * j + grp;
+          live[j] = slot < s.total && slot >= s.lo;
+          int page = -1;
+          if (live[j]) {
+            page = page_of(a.pg, table, slot);
+            if (page < 0) {
+              live[j] = false;
+              if (l8 == 0) pages_report(a.pg, BAD_ID);
+            }
+          }
+          const long long at = live[j] ? slot_offset(a.pg, page, h, slot) : 0;
+          struct alignas(V * sizeof(T)) Load { T v[V]; };
+#pragma unroll
+          for (int n = 0; n < NV; ++n) {
+            Load ld_k{}, ld_v{};
+            if (live[j]) {
+              ld_k = *reinterpret_cast<const Load *>(a.pg.k + at + (n * 8 + l8) * V * sizeof(T));
+              ld_v = *reinterpret_cast<const Load *>(a.pg.v + at + (n * 8 + l8) * V * sizeof(T));
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) kx[j][n * V + e] = ld_k.v[e], vx[j][n * V + e] = ld_v.v[e];
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+          float sc[KEYS], top = m[r];
+#pragma unroll
+          for (int j = 0; j < KEYS; ++j) {
+            float d = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) d = fmaf(q[r][e], to_f32(kx[j][e]), d);
+            d += __shfl_xor_sync(0xffffffffu, d, 1);
+            d += __shfl_xor_sync(0xffffffffu, d, 2);
+            d += __shfl_xor_sync(0xffffffffu, d, 4);
+            const int slot = base + i + 4 * j + grp;
+            sc[j] = live[j] && slot >= range[r].x && slot < range[r].y ? d * a.scale2 : -INFINITY;
+            top = fmaxf(top, sc[j]);
+            if (a.scores && l8 == 0 && r < rows && slot < s.total)
+              a.scores[(((long long)run.b * a.pg.n_kv_heads + h) * a.M * a.group + row0 + r) * a.score_stride + slot] = sc[j];
+          }
+          const float ref = top == -INFINITY ? 0.f : top, corr = exp2f(m[r] - ref);
+          float p[KEYS], sum = 0.f;
+#pragma unroll
+          for (int j = 0; j < KEYS; ++j) sum += p[j] = exp2f(sc[j] - ref);
+          m[r] = top;
+          l[r] = fmaf(l[r], corr, sum);
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            float v = o[r][e] * corr;
+            // (a slot that this row does not see may hold anything: 0 x NaN must not happen)
+#pragma unroll
+            for (int j = 0; j < KEYS; ++j) v = sc[j] == -INFINITY ? v : fmaf(p[j], to_f32(vx[j][e]), v);
+            o[r][e] = v;
+          }
+        }
+      }
+    }
+    // the four groups of a warp, then the warps
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+      for (int x = 8; x < 32; x <<= 1) {
+        const float om = __shfl_xor_sync(0xffffffffu, m[r], x), ol = __shfl_xor_sync(0xffffffffu, l[r], x);
+        const float top = fmaxf(m[r], om), ref = top == -INFINITY ? 0.f : top;
+        const float f0 = exp2f(m[r] - ref), f1 = exp2f(om - ref);
+        m[r] = top;
+        l[r] = l[r] * f0 + ol * f1;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[r][e] = o[r][e] * f0 + __shfl_xor_sync(0xffffffffu, o[r][e], x) * f1;
+      }
+      if (grp == 0) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) s_o[warp][r][e / V * 8 * V + l8 * V + e % V] = o[r][e];
+        if (l8 == 0) s_ml[warp][r] = make_float2(m[r], l[r]);
+      }
+    }
+    __syncthreads();
+    const bool whole = run.first == 0 && take == s.tiles;
+    const int part = 2 * blockIdx.x + (run.first == 0);
+    for (int i = threadIdx.x; i < rows * D; i += PA_THREADS) {
+      const int r = i / D, d = i - r * D;
+      float top = s_ml[0][r].x;
+#pragma unroll
+      for (int w = 1; w < WARPS; ++w) top = fmaxf(top, s_ml[w][r].x);
+      const float ref = top == -INFINITY ? 0.f : top;
+      float sum = 0.f, v = 0.f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        const float f = exp2f(s_ml[w][r].x - ref);
+        sum = fmaf(s_ml[w][r].y, f, sum);
+        v = fmaf(s_o[w][r][d], f, v);
+      }
+      if (whole) {
+        if ((row0 + r) / a.group < s.n_new) {
+          paged_out_row<T>(a, run.b, h, row0 + r, D)[d] = from_f32<T>(sum == 0.f ? 0.f : v / sum);
+          if (d == 0) paged_write_lse(a, run.b, h, row0 + r, top, sum);
+        }
+      } else {
+        a.part_o[((long long)part * ROWS + r) * D + d] = v;
+        if (d == 0) a.part_ml[part * ROWS + r] = make_float2(top, sum);
+      }
+    }
+    __syncthreads();
+    run.count -= take;
+    run.first = 0;
+    if (++run.u == a.units) run.u = 0, ++run.b;
+  }
+}
+
+// Joins the parts of the units that several CTAs shared: block x belongs to CTA x of the kernel before and works if that one is
+// the second of a unit's CTAs.  A warp a row.
+template <typename T, int D>
+__global__ void __launch_bounds__(32 * PA_JOIN_WARPS) paged_join_kernel(const __grid_constant__ PagedAttnArgs a, int ROWS) {
+  constexpr int E = D / 32;
+  pdl_sync();
+  const PagedMeta meta = a.meta[blockIdx.x];
+  if (meta.b < 0 || meta.c0 + 1 != (int)blockIdx.x) return;
+  const int lane = threadIdx.x & 31, r = blockIdx.y * PA_JOIN_WARPS + (threadIdx.x >> 5);
+  const int h = meta.u / a.chunks, row = (meta.u - h * a.chunks) * ROWS + r;
+  if (r >= ROWS || row >= a.M * a.group) return;
+  if (row / a.group >= (a.n_new ? cut(a.n_new[meta.b], a.M) : a.M)) return;
+  const int parts = meta.c1 - meta.c0 + 1;
+  auto index = [&](int i) { return (long long)(i == 0 ? 2 * meta.c0 + 1 : 2 * (meta.c0 + i)) * ROWS + r; };
+  float top = -INFINITY;
+  for (int i = lane; i < parts; i += 32) top = fmaxf(top, a.part_ml[index(i)].x);
+  top = warp_max(top);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f, o[E] = {};
+#pragma unroll 4
+  for (int i = 0; i < parts; ++i) {
+    const float2 ml = a.part_ml[index(i)];
+    const float f = exp2f(ml.x - ref);
+    sum = fmaf(ml.y, f, sum);
+    const float *src = a.part_o + index(i) * D + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(src[e], f, o[e]);
+  }
+  T *out = paged_out_row<T>(a, meta.b, h, row, D) + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) out[e] = from_f32<T>(sum == 0.f ? 0.f : o[e] / sum);
+  if (lane == 0) paged_write_lse(a, meta.b, h, row, top, sum);
+}
+
+// w_out = w_in + sum over the rows of 2^(score - lse2): a thread a slot.
+__global__ void __launch_bounds__(256) paged_weights_kernel(const __grid_constant__ PagedAttnArgs a) {
+  pdl_wait();
+  const int Hkv = a.pg.n_kv_heads, b = blockIdx.x / Hkv, R = a.M * a.group;
+  const PagedSpan s = paged_span(a, b, false);
+  const float *w_in = a.w_in ? a.w_in + blockIdx.x * a.w_stride : nullptr;
+  float *w_out = a.w_out + blockIdx.x * a.w_stride;
+  for (int slot = blockIdx.y * 256 + threadIdx.x; slot < s.total; slot += gridDim.y * 256) {
+    float w = w_in ? w_in[slot] : 0.f;
+    for (int m = 0; m < s.n_new; ++m) {
+      const int2 range = paged_row_range(a, s, m);
+      if (slot < range.x || slot >= range.y) continue;
+      for (int g = 0; g < a.group; ++g) {
+        const long long row = (long long)blockIdx.x * R + m * a.group + g;
+        const float lse2 = a.lse2[row];
+        if (lse2 != -INFINITY) w += exp2f(a.scores[row * a.score_stride + slot] - lse2);
+      }
+    }
+    w_out[slot] = w;
+  }
+}
+
+}  // namespace tsfm

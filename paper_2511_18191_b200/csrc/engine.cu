@@ -1797,3 +1797,5 @@ const char *tsfm_strerror(int code) {
 const char *tsfm_last_cuda_error(void) { return g_cuda_err.c_str(); }
 
 }  // extern "C"
+
+#include "serving.cuh"

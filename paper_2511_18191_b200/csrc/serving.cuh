@@ -1,0 +1,311 @@
+// C entry points for serving over a cache of pages (the section of that name in include/tsfm.h): argument checks, launch
+// shapes, workspace layout.
+#pragma once
+#include "attn_paged.cuh"
+#include "cache_evict.cuh"
+#include "pages.cuh"
+#include "rope_append.cuh"
+#include "verify_tokens.cuh"
+
+namespace {
+
+constexpr int kSms = 148;
+constexpr long long kMaxSlots = 1 << 30;           // of a series: slot arithmetic is 32-bit
+constexpr long long kMaxGridX = 0x7fffffff;
+
+bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+bool stride_ok(int64_t stride, int64_t least, int e) { return stride >= least && stride <= (INT64_MAX >> 4) && stride * e % 16 == 0; }
+
+int pages_shape(const tsfm_kv_pages *p) {
+  if (!p || (p->dtype != TSFM_F32 && p->dtype != TSFM_BF16) || p->n_kv_heads < 1) return TSFM_ERR_ARG;
+  if (p->d_head != 32 && p->d_head != 64 && p->d_head != 128) return TSFM_ERR_SHAPE;
+  return TSFM_OK;
+}
+
+int pages_init(PagesDev *d, const tsfm_kv_pages *p) {
+  if (int rc = pages_shape(p)) return rc;
+  if (!p->k || !p->v || !p->table || p->max_pages < 1 || p->table_stride < p->max_pages || p->n_pages < 1 || p->page_size < 1)
+    return TSFM_ERR_ARG;
+  const int e = (int)elt_bytes(p->dtype);
+  if (p->page_size > 65536 || (p->page_size & (p->page_size - 1))) return TSFM_ERR_SHAPE;
+  if (!aligned16(p->k) || !aligned16(p->v) || !stride_ok(p->page_stride, p->d_head, e) || !stride_ok(p->head_stride, p->d_head, e) ||
+      !stride_ok(p->slot_stride, p->d_head, e))
+    return TSFM_ERR_SHAPE;
+  d->k = (char *)p->k;
+  d->v = (char *)p->v;
+  d->page_stride = p->page_stride * e;
+  d->head_stride = p->head_stride * e;
+  d->slot_stride = p->slot_stride * e;
+  d->table = p->table;
+  d->table_stride = p->table_stride;
+  d->n_pages = p->n_pages;
+  for (d->page_log = 0; 1 << d->page_log < p->page_size;) ++d->page_log;
+  d->n_kv_heads = p->n_kv_heads;
+  d->capacity = (int)std::min<long long>(kMaxSlots, (long long)p->max_pages * p->page_size);
+  d->status = p->status;
+  return TSFM_OK;
+}
+
+template <typename... KArgs, typename... Args>
+cudaError_t launch_after(cudaStream_t s, dim3 grid, int threads, void (*kernel)(KArgs...), const Args &...args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
+
+// The workspace of tsfm_paged_attention: rows of a unit, CTAs, and where the parts of it begin.
+struct PagedPlan {
+  int rows, chunks, grid;
+  size_t part_ml, part_o, lse2, scores, bytes;
+  long long score_stride;
+};
+int paged_plan(PagedPlan *pl, const tsfm_kv_pages *p, int B, int M, int n_heads, int max_len, bool weights) {
+  if (int rc = pages_shape(p)) return rc;
+  if (B < 1 || M < 1 || n_heads < 1 || max_len < 1) return TSFM_ERR_ARG;
+  if (n_heads % p->n_kv_heads) return TSFM_ERR_SHAPE;
+  const long long R = (long long)M * (n_heads / p->n_kv_heads), pairs = (long long)B * p->n_kv_heads;
+  if (max_len > kMaxSlots || R > 1 << 20 || pairs > kMaxGridX || (long long)B * M > kMaxGridX) return TSFM_ERR_SHAPE;
+  pl->rows = R == 1 ? 1 : R == 2 ? 2 : 4;
+  pl->chunks = (int)((R + pl->rows - 1) / pl->rows);
+  if (pairs * pl->chunks > kMaxGridX) return TSFM_ERR_SHAPE;
+  const long long tiles = pairs * pl->chunks * ((max_len + PA_TILE - 1) / PA_TILE);
+  pl->grid = (int)std::min<long long>(tiles, 4 * kSms);
+  size_t at = align256(sizeof(PagedMeta) * pl->grid);
+  auto take = [&](size_t bytes) { const size_t o = at; at = align256(at + bytes); return o; };
+  pl->part_ml = take(sizeof(float2) * 2 * pl->grid * pl->rows);
+  pl->part_o = take(sizeof(float) * 2 * pl->grid * pl->rows * p->d_head);
+  pl->score_stride = ((long long)max_len + 31) / 32 * 32;
+  pl->lse2 = weights ? take(sizeof(float) * pairs * R) : 0;
+  pl->scores = weights ? take(sizeof(float) * pairs * R * pl->score_stride) : 0;
+  pl->bytes = at;
+  return TSFM_OK;
+}
+
+template <typename T, int D>
+cudaError_t launch_paged(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl) {
+  switch (pl.rows) {
+    case 1: paged_attn_fma_kernel<T, D, 1><<<pl.grid, PA_THREADS, 0, s>>>(a); break;
+    case 2: paged_attn_fma_kernel<T, D, 2><<<pl.grid, PA_THREADS, 0, s>>>(a); break;
+    default: paged_attn_fma_kernel<T, D, 4><<<pl.grid, PA_THREADS, 0, s>>>(a);
+  }
+  if (cudaError_t e = cudaGetLastError()) return e;
+  LAUNCHED();
+  if (pl.grid > 1) {
+    if (cudaError_t e = launch_after(s, dim3(pl.grid, (pl.rows + PA_JOIN_WARPS - 1) / PA_JOIN_WARPS), 32 * PA_JOIN_WARPS, paged_join_kernel<T, D>, a, pl.rows)) return e;
+    LAUNCHED();
+  }
+  if (a.w_out) {
+    const long long chunks = (a.pg.capacity + 255ll) / 256;
+    if (cudaError_t e = launch_after(s, dim3((unsigned)(a.B * a.pg.n_kv_heads), (unsigned)std::min(chunks, 4096ll)), 256, paged_weights_kernel, a)) return e;
+    LAUNCHED();
+  }
+  return cudaSuccess;
+}
+
+}  // namespace
+
+extern "C" {
+
+int tsfm_rope_init(tsfm_rope *rope, int32_t layout, int32_t rot_dim, int32_t scaling, double base, double factor,
+                   double original_len, double turns_lo, double turns_hi, float mscale) {
+  if (!rope || (layout != TSFM_ROPE_HALF && layout != TSFM_ROPE_INTERLEAVED) || scaling < TSFM_ROPE_PLAIN || scaling > TSFM_ROPE_PARTS)
+    return TSFM_ERR_ARG;
+  if (rot_dim < 0 || rot_dim > 2 * ROPE_MAX_PAIRS || rot_dim % 2) return TSFM_ERR_ARG;
+  if (!(base > 1) || !std::isfinite(base) || !(factor >= 1) || !std::isfinite(factor) || !std::isfinite(mscale)) return TSFM_ERR_ARG;
+  if (scaling == TSFM_ROPE_BASE && rot_dim == 2) return TSFM_ERR_ARG;
+  if (scaling == TSFM_ROPE_PARTS && (!(original_len > 0) || !std::isfinite(original_len) || !(turns_lo >= 0) || !(turns_hi > turns_lo) || !std::isfinite(turns_hi)))
+    return TSFM_ERR_ARG;
+  std::memset(rope, 0, sizeof *rope);
+  rope->layout = layout;
+  rope->rot_dim = rot_dim;
+  rope->mscale = mscale;
+  const long double two_pi = 6.283185307179586476925286766559L;
+  long double b = base;
+  if (scaling == TSFM_ROPE_BASE && rot_dim > 2) b *= powl(factor, rot_dim / (rot_dim - 2.0L));
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    long double f = powl(b, -2.0L * i / rot_dim);
+    if (scaling == TSFM_ROPE_LINEAR) f /= factor;
+    if (scaling == TSFM_ROPE_PARTS) {
+      long double g = (original_len * f / two_pi - turns_lo) / ((long double)turns_hi - turns_lo);
+      g = g < 0 ? 0 : g > 1 ? 1 : g;
+      f *= g + (1 - g) / factor;
+    }
+    rope->turn[i] = (uint64_t)(f / two_pi * 18446744073709551616.0L + 0.5L);       // f <= 1: below 2^62
+  }
+  return TSFM_OK;
+}
+
+int tsfm_rope_append(void *stream, const tsfm_rope *rope, const tsfm_kv_pages *pages, const void *qkv, int64_t qkv_stride,
+                     void *q_out, int64_t q_out_stride, const int32_t *pos, const int32_t *len, const int32_t *n_new,
+                     int32_t B, int32_t M, int32_t n_heads) {
+  if (!rope || !qkv || !len || B < 1 || M < 1 || n_heads < 0 || (q_out && n_heads < 1)) return TSFM_ERR_ARG;
+  if ((rope->layout != TSFM_ROPE_HALF && rope->layout != TSFM_ROPE_INTERLEAVED) || rope->rot_dim < 0 || rope->rot_dim % 2) return TSFM_ERR_ARG;
+  RopeAppendArgs a{};
+  if (int rc = pages_init(&a.pg, pages)) return rc;
+  const int D = pages->d_head, e = (int)elt_bytes(pages->dtype);
+  const int64_t row = ((int64_t)n_heads + 2ll * pages->n_kv_heads) * D;
+  if (rope->rot_dim > D || (int64_t)B * M > kMaxGridX) return TSFM_ERR_SHAPE;
+  if (!aligned16(qkv) || !stride_ok(qkv_stride, row, e)) return TSFM_ERR_SHAPE;
+  if (q_out && (!aligned16(q_out) || !stride_ok(q_out_stride, (int64_t)n_heads * D, e))) return TSFM_ERR_SHAPE;
+  if (q_out == qkv && q_out_stride != qkv_stride) return TSFM_ERR_ARG;
+  a.qkv = qkv;
+  a.q_out = q_out;
+  a.qkv_stride = qkv_stride;
+  a.q_stride = q_out_stride;
+  a.pos = pos;
+  a.len = len;
+  a.n_new = n_new;
+  a.tokens = B * M;
+  a.M = M;
+  a.n_heads = n_heads;
+  a.half = rope->layout == TSFM_ROPE_HALF;
+  a.pairs = rope->rot_dim / 2;
+  a.mscale = rope->mscale;
+  std::memcpy(a.turn, rope->turn, sizeof a.turn);
+  if (pages->dtype == TSFM_BF16) launch_rope_append<bf16>((cudaStream_t)stream, a, D);
+  else launch_rope_append<float>((cudaStream_t)stream, a, D);
+  CU_TRY(cudaGetLastError());
+  LAUNCHED();
+  return TSFM_OK;
+}
+
+size_t tsfm_paged_attention_workspace(const tsfm_kv_pages *pages, int32_t B, int32_t M, int32_t n_heads, int32_t max_len,
+                                      int32_t with_weights) {
+  PagedPlan pl;
+  return paged_plan(&pl, pages, B, M, n_heads, max_len, with_weights != 0) ? 0 : pl.bytes;
+}
+
+int tsfm_paged_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                         const int32_t *len, const int32_t *n_new, int32_t B, int32_t M, int32_t n_heads, float scale,
+                         int32_t causal, int32_t window, int32_t max_len, float *lse, const float *w_in, float *w_out,
+                         int64_t w_stride, void *workspace, size_t workspace_bytes) {
+  if (!q || !out || !len || !workspace || window < 0 || !std::isfinite(scale) || (w_in && !w_out)) return TSFM_ERR_ARG;
+  PagedPlan pl;
+  if (int rc = paged_plan(&pl, pages, B, M, n_heads, max_len, w_out != nullptr)) return rc;
+  PagedAttnArgs a{};
+  if (int rc = pages_init(&a.pg, pages)) return rc;
+  const int D = pages->d_head, e = (int)elt_bytes(pages->dtype);
+  const int64_t row = (int64_t)n_heads * D;
+  if (!aligned16(q) || !aligned16(out) || !stride_ok(q_stride, row, e) || !stride_ok(out_stride, row, e)) return TSFM_ERR_SHAPE;
+  if (w_out && w_stride < max_len) return TSFM_ERR_SHAPE;
+  if ((uintptr_t)workspace & 255 || workspace_bytes < pl.bytes) return TSFM_ERR_SHAPE;
+  a.pg.capacity = std::min(a.pg.capacity, max_len);
+  a.q = q;
+  a.out = out;
+  a.q_stride = q_stride;
+  a.out_stride = out_stride;
+  a.len = len;
+  a.n_new = n_new;
+  a.B = B;
+  a.M = M;
+  a.n_heads = n_heads;
+  a.group = n_heads / pages->n_kv_heads;
+  a.scale2 = scale * 1.4426950408889634f;
+  a.causal = causal != 0;
+  a.window = window;
+  a.lse = lse;
+  a.w_in = w_in;
+  a.w_out = w_out;
+  a.w_stride = w_stride;
+  a.chunks = pl.chunks;
+  a.units = pages->n_kv_heads * pl.chunks;
+  char *ws = (char *)workspace;
+  a.meta = (PagedMeta *)ws;
+  a.part_ml = (float2 *)(ws + pl.part_ml);
+  a.part_o = (float *)(ws + pl.part_o);
+  a.lse2 = w_out ? (float *)(ws + pl.lse2) : nullptr;
+  a.scores = w_out ? (float *)(ws + pl.scores) : nullptr;
+  a.score_stride = pl.score_stride;
+  cudaStream_t s = (cudaStream_t)stream;
+  cudaError_t err;
+  if (pages->dtype == TSFM_BF16)
+    err = D == 32 ? launch_paged<bf16, 32>(s, a, pl) : D == 64 ? launch_paged<bf16, 64>(s, a, pl) : launch_paged<bf16, 128>(s, a, pl);
+  else
+    err = D == 32 ? launch_paged<float, 32>(s, a, pl) : D == 64 ? launch_paged<float, 64>(s, a, pl) : launch_paged<float, 128>(s, a, pl);
+  CU_TRY(err);
+  return TSFM_OK;
+}
+
+int tsfm_cache_evict(void *stream, const tsfm_kv_pages *pages, const int32_t *dst_table, int32_t dst_stride, const int32_t *len,
+                     const float *w, int64_t w_stride, int32_t B, int32_t budget, int32_t sinks, int32_t recent, int32_t max_len,
+                     int32_t *kept, float *w_out, int64_t w_out_stride, int32_t *len_out) {
+  if (!dst_table || !len || !w || !kept || !len_out || len == len_out || w == w_out) return TSFM_ERR_ARG;
+  if (B < 1 || budget < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget || max_len < 1) return TSFM_ERR_ARG;
+  EvictArgs a{};
+  if (int rc = pages_init(&a.pg, pages)) return rc;
+  a.pg.capacity = std::min(a.pg.capacity, max_len);
+  const long long pairs = (long long)B * pages->n_kv_heads, most = std::min(budget, a.pg.capacity);
+  if (pairs > kMaxGridX || w_stride < a.pg.capacity || (w_out && w_out_stride < most)) return TSFM_ERR_SHAPE;
+  if ((long long)dst_stride * pages->page_size < most) return TSFM_ERR_SHAPE;
+  a.dst_table = dst_table;
+  a.dst_stride = dst_stride;
+  a.len = len;
+  a.w = w;
+  a.w_stride = w_stride;
+  a.w_out_stride = w_out_stride;
+  a.B = B;
+  a.budget = budget;
+  a.sinks = sinks;
+  a.recent = recent;
+  a.kept = kept;
+  a.w_out = w_out;
+  a.len_out = len_out;
+  a.vecs = pages->d_head * (int)elt_bytes(pages->dtype) / 16;
+  cudaStream_t s = (cudaStream_t)stream;
+  evict_select_kernel<<<(unsigned)pairs, EVICT_THREADS, 0, s>>>(a);
+  CU_TRY(cudaGetLastError());
+  LAUNCHED();
+  const long long rows = 256 / a.vecs * EVICT_ROWS, chunks = (most + rows - 1) / rows;
+  CU_TRY(launch_after(s, dim3((unsigned)pairs, (unsigned)std::min(chunks, 65535ll)), 256, evict_copy_kernel, a));
+  LAUNCHED();
+  return TSFM_OK;
+}
+
+int tsfm_verify_tokens(void *stream, const int32_t *tokens, const float *p, int64_t p_stride, const float *q, int64_t q_stride,
+                       int32_t B, int32_t K, int32_t V, const float *u, uint64_t seed, int32_t round_idx, int32_t series0,
+                       const int32_t *n_draft, const int32_t *len, int32_t *out, int32_t *n_accept, int32_t *len_out) {
+  if (!p || !out || !n_accept || B < 1 || K < 0 || K > TSFM_MAX_K || V < 1 || (K && !tokens) || !len != !len_out) return TSFM_ERR_ARG;
+  if (p_stride < V || (q && q_stride < V)) return TSFM_ERR_ARG;
+  VerifyArgs a{};
+  a.tokens = tokens;
+  a.p = p;
+  a.q = q;
+  a.p_stride = p_stride;
+  a.q_stride = q_stride;
+  a.K = K;
+  a.V = V;
+  a.u = u;
+  a.key = make_uint2((uint32_t)(seed & 0xffffffffu), (uint32_t)(seed >> 32));
+  a.round_idx = round_idx;
+  a.series0 = series0;
+  a.n_draft = n_draft;
+  a.len = len;
+  a.out = out;
+  a.n_accept = n_accept;
+  a.len_out = len_out;
+  int cluster = 1;
+  while (cluster < VERIFY_MAX_CLUSTER && (long long)B * cluster < 2 * kSms && V / cluster > 4096) cluster *= 2;
+  if ((long long)B * cluster > kMaxGridX) return TSFM_ERR_SHAPE;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(B * cluster));
+  cfg.blockDim = dim3(VERIFY_THREADS);
+  cfg.stream = (cudaStream_t)stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = cluster;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  CU_TRY(cudaLaunchKernelEx(&cfg, verify_tokens_kernel, a));
+  LAUNCHED();
+  return TSFM_OK;
+}
+
+}  // extern "C"
