@@ -13,6 +13,7 @@ namespace tsfm {
 constexpr int PA_TILE = 64;                        // slots
 constexpr int PA_THREADS = 128;
 constexpr int PA_JOIN_WARPS = 4;
+constexpr int PA_F32_CTAS = 4;                     // on an SM
 
 // What a CTA that starts inside a unit leaves for the join: the unit, and the CTAs that share it.
 struct PagedMeta {
@@ -125,11 +126,11 @@ __device__ __forceinline__ T *paged_out_row(const PagedAttnArgs &a, int b, int h
   return reinterpret_cast<T *>(a.out) + ((long long)b * a.M + tok) * a.out_stride + (long long)head * D;
 }
 
-// The FMA kernel.  Eight lanes share a slot, a warp works on four at a time, each group of eight lanes with its own running
+// The fp32 kernel.  Eight lanes share a slot, a warp works on four at a time, each group of eight lanes with its own running
 // maximum and sum; nothing is staged.
-template <typename T, int D, int ROWS>
-__global__ void __launch_bounds__(PA_THREADS) paged_attn_fma_kernel(const __grid_constant__ PagedAttnArgs a) {
-  constexpr int E = D / 8, V = Pack16<T>::N < E ? Pack16<T>::N : E, NV = E / V;       // elements a lane, of a load, loads
+template <int D, int ROWS>
+__global__ void __launch_bounds__(PA_THREADS) paged_attn_f32_kernel(const __grid_constant__ PagedAttnArgs a) {
+  constexpr int E = D / 8, V = 4, NV = E / V;                                       // elements a lane, of a load, loads
   constexpr int WARPS = PA_THREADS / 32, KEYS = 2;                                  // slots of a group in flight
   __shared__ float s_o[WARPS][ROWS][D];
   __shared__ float2 s_ml[WARPS][ROWS];
@@ -160,18 +161,18 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_fma_kernel(const __grid
       l[r] = 0.f;
       range[r] = r < rows ? paged_row_range(a, s, (row0 + r) / a.group) : make_int2(0, 0);
       const int tok = r < rows ? (row0 + r) / a.group : 0, head = h * a.group + (r < rows ? row0 + r - tok * a.group : 0);
-      const T *src = reinterpret_cast<const T *>(a.q) + ((long long)run.b * a.M + tok) * a.q_stride + (long long)head * D;
+      const float *src = reinterpret_cast<const float *>(a.q) + ((long long)run.b * a.M + tok) * a.q_stride + (long long)head * D;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         o[r][e] = 0.f;
-        q[r][e] = to_f32(src[e / V * 8 * V + l8 * V + e % V]);
+        q[r][e] = src[e / V * 8 * V + l8 * V + e % V];
       }
     }
     for (int t = run.first; t < run.first + take; ++t) {
       const int base = (s.tile0 + t) * PA_TILE + warp * (PA_TILE / WARPS);
 #pragma unroll 1
       for (int i = 0; i < PA_TILE / WARPS; i += 4 * KEYS) {
-        T kx[KEYS][E], vx[KEYS][E];
+        float kx[KEYS][E], vx[KEYS][E];
         bool live[KEYS];
 #pragma unroll
         for (int j = 0; j < KEYS; ++j) {
@@ -186,16 +187,15 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_fma_kernel(const __grid
             }
           }
           const long long at = live[j] ? slot_offset(a.pg, page, h, slot) : 0;
-          struct alignas(V * sizeof(T)) Load { T v[V]; };
 #pragma unroll
           for (int n = 0; n < NV; ++n) {
-            Load ld_k{}, ld_v{};
+            float4 k4 = make_float4(0.f, 0.f, 0.f, 0.f), v4 = k4;
             if (live[j]) {
-              ld_k = *reinterpret_cast<const Load *>(a.pg.k + at + (n * 8 + l8) * V * sizeof(T));
-              ld_v = *reinterpret_cast<const Load *>(a.pg.v + at + (n * 8 + l8) * V * sizeof(T));
+              k4 = *reinterpret_cast<const float4 *>(a.pg.k + at + (n * 8 + l8) * 16);
+              v4 = *reinterpret_cast<const float4 *>(a.pg.v + at + (n * 8 + l8) * 16);
             }
-#pragma unroll
-            for (int e = 0; e < V; ++e) kx[j][n * V + e] = ld_k.v[e], vx[j][n * V + e] = ld_v.v[e];
+            kx[j][n * V] = k4.x, kx[j][n * V + 1] = k4.y, kx[j][n * V + 2] = k4.z, kx[j][n * V + 3] = k4.w;
+            vx[j][n * V] = v4.x, vx[j][n * V + 1] = v4.y, vx[j][n * V + 2] = v4.z, vx[j][n * V + 3] = v4.w;
           }
         }
 #pragma unroll
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_fma_kernel(const __grid
           for (int j = 0; j < KEYS; ++j) {
             float d = 0.f;
 #pragma unroll
-            for (int e = 0; e < E; ++e) d = fmaf(q[r][e], to_f32(kx[j][e]), d);
+            for (int e = 0; e < E; ++e) d = fmaf(q[r][e], kx[j][e], d);
             d += __shfl_xor_sync(0xffffffffu, d, 1);
             d += __shfl_xor_sync(0xffffffffu, d, 2);
             d += __shfl_xor_sync(0xffffffffu, d, 4);
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_fma_kernel(const __grid
             float v = o[r][e] * corr;
             // (a slot that this row does not see may hold anything: 0 x NaN must not happen)
 #pragma unroll
-            for (int j = 0; j < KEYS; ++j) v = sc[j] == -INFINITY ? v : fmaf(p[j], to_f32(vx[j][e]), v);
+            for (int j = 0; j < KEYS; ++j) v = sc[j] == -INFINITY ? v : fmaf(p[j], vx[j][e], v);
             o[r][e] = v;
           }
         }
@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_fma_kernel(const __grid
       }
       if (whole) {
         if ((row0 + r) / a.group < s.n_new) {
-          paged_out_row<T>(a, run.b, h, row0 + r, D)[d] = from_f32<T>(sum == 0.f ? 0.f : v / sum);
+          paged_out_row<float>(a, run.b, h, row0 + r, D)[d] = sum == 0.f ? 0.f : v / sum;
           if (d == 0) paged_write_lse(a, run.b, h, row0 + r, top, sum);
         }
       } else {

@@ -2,6 +2,7 @@
 // shapes, workspace layout.
 #pragma once
 #include "attn_paged.cuh"
+#include "attn_paged_mma.cuh"
 #include "cache_evict.cuh"
 #include "pages.cuh"
 #include "rope_append.cuh"
@@ -72,11 +73,21 @@ int paged_plan(PagedPlan *pl, const tsfm_kv_pages *p, int B, int M, int n_heads,
   if (n_heads % p->n_kv_heads) return TSFM_ERR_SHAPE;
   const long long R = (long long)M * (n_heads / p->n_kv_heads), pairs = (long long)B * p->n_kv_heads;
   if (max_len > kMaxSlots || R > 1 << 20 || pairs > kMaxGridX || (long long)B * M > kMaxGridX) return TSFM_ERR_SHAPE;
-  pl->rows = R == 1 ? 1 : R == 2 ? 2 : 4;
+  // rows of a unit: fp32 what a thread's registers hold, bf16 16 to a warp
+  int ctas = PA_F32_CTAS;
+  if (p->dtype == TSFM_BF16) {
+    pl->rows = R <= 16 ? 16 : R <= 32 ? 32 : 64;
+    auto of = [&](auto one, auto two, auto four) { return R <= 16 ? decltype(one)::CTAS : R <= 32 ? decltype(two)::CTAS : decltype(four)::CTAS; };
+    ctas = p->d_head == 32   ? of(PagedMma<32, 1>(), PagedMma<32, 2>(), PagedMma<32, 4>())
+           : p->d_head == 64 ? of(PagedMma<64, 1>(), PagedMma<64, 2>(), PagedMma<64, 4>())
+                             : of(PagedMma<128, 1>(), PagedMma<128, 2>(), PagedMma<128, 4>());
+  } else {
+    pl->rows = R == 1 ? 1 : R == 2 ? 2 : 4;
+  }
   pl->chunks = (int)((R + pl->rows - 1) / pl->rows);
   if (pairs * pl->chunks > kMaxGridX) return TSFM_ERR_SHAPE;
   const long long tiles = pairs * pl->chunks * ((max_len + PA_TILE - 1) / PA_TILE);
-  pl->grid = (int)std::min<long long>(tiles, 4 * kSms);
+  pl->grid = (int)std::min<long long>(tiles, (long long)ctas * kSms);
   size_t at = align256(sizeof(PagedMeta) * pl->grid);
   auto take = [&](size_t bytes) { const size_t o = at; at = align256(at + bytes); return o; };
   pl->part_ml = take(sizeof(float2) * 2 * pl->grid * pl->rows);
@@ -88,14 +99,31 @@ int paged_plan(PagedPlan *pl, const tsfm_kv_pages *p, int B, int M, int n_heads,
   return TSFM_OK;
 }
 
+template <int D, int WR>
+cudaError_t launch_paged_mma(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl) {
+  using C = PagedMma<D, WR>;
+  // (the attribute belongs to the device's context: set with every call, 0.2 us)
+  if (cudaError_t e = cudaFuncSetAttribute(paged_attn_mma_kernel<D, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES)) return e;
+  paged_attn_mma_kernel<D, WR><<<pl.grid, PA_THREADS, C::SMEM_BYTES, s>>>(a);
+  return cudaGetLastError();
+}
+template <int D>
+cudaError_t launch_paged_rows(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl, bf16) {
+  return pl.rows == 16 ? launch_paged_mma<D, 1>(s, a, pl) : pl.rows == 32 ? launch_paged_mma<D, 2>(s, a, pl) : launch_paged_mma<D, 4>(s, a, pl);
+}
+template <int D>
+cudaError_t launch_paged_rows(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl, float) {
+  switch (pl.rows) {
+    case 1: paged_attn_f32_kernel<D, 1><<<pl.grid, PA_THREADS, 0, s>>>(a); break;
+    case 2: paged_attn_f32_kernel<D, 2><<<pl.grid, PA_THREADS, 0, s>>>(a); break;
+    default: paged_attn_f32_kernel<D, 4><<<pl.grid, PA_THREADS, 0, s>>>(a);
+  }
+  return cudaGetLastError();
+}
+
 template <typename T, int D>
 cudaError_t launch_paged(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl) {
-  switch (pl.rows) {
-    case 1: paged_attn_fma_kernel<T, D, 1><<<pl.grid, PA_THREADS, 0, s>>>(a); break;
-    case 2: paged_attn_fma_kernel<T, D, 2><<<pl.grid, PA_THREADS, 0, s>>>(a); break;
-    default: paged_attn_fma_kernel<T, D, 4><<<pl.grid, PA_THREADS, 0, s>>>(a);
-  }
-  if (cudaError_t e = cudaGetLastError()) return e;
+  if (cudaError_t e = launch_paged_rows<D>(s, a, pl, T())) return e;
   LAUNCHED();
   if (pl.grid > 1) {
     if (cudaError_t e = launch_after(s, dim3(pl.grid, (pl.rows + PA_JOIN_WARPS - 1) / PA_JOIN_WARPS), 32 * PA_JOIN_WARPS, paged_join_kernel<T, D>, a, pl.rows)) return e;
