@@ -12,7 +12,7 @@ namespace tsfm {
 
 constexpr int PA_TILE = 64;                        // slots
 constexpr int PA_THREADS = 128;
-constexpr int PA_JOIN_WARPS = 4;
+constexpr int PA_JOIN_WARPS = 8;
 constexpr int PA_F32_CTAS = 4;                     // on an SM
 
 // What a CTA that starts inside a unit leaves for the join: the unit, and the CTAs that share it.
@@ -285,37 +285,68 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_f32_kernel(const __grid
 }
 
 // Joins the parts of the units that several CTAs shared: block x belongs to CTA x of the kernel before and works if that one is
-// the second of a unit's CTAs.  A warp a row.
+// the second of a unit's CTAs; block y is a row.  The warps share the parts: with one warp a row the 37 parts of
+// one series of 131071 slots (D 128) were a chain of loads as long as a third of the kernel before.
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * PA_JOIN_WARPS) paged_join_kernel(const __grid_constant__ PagedAttnArgs a, int ROWS) {
-  constexpr int E = D / 32;
+  constexpr int E = D / 32, W = PA_JOIN_WARPS;
+  __shared__ float s_o[W][D];
+  __shared__ float2 s_ml[W];
   pdl_sync();
   const PagedMeta meta = a.meta[blockIdx.x];
   if (meta.b < 0 || meta.c0 + 1 != (int)blockIdx.x) return;
-  const int lane = threadIdx.x & 31, r = blockIdx.y * PA_JOIN_WARPS + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = blockIdx.y;
   const int h = meta.u / a.chunks, row = (meta.u - h * a.chunks) * ROWS + r;
-  if (r >= ROWS || row >= a.M * a.group) return;
-  if (row / a.group >= (a.n_new ? cut(a.n_new[meta.b], a.M) : a.M)) return;
+  if (row >= a.M * a.group || row / a.group >= (a.n_new ? cut(a.n_new[meta.b], a.M) : a.M)) return;
   const int parts = meta.c1 - meta.c0 + 1;
   auto index = [&](int i) { return (long long)(i == 0 ? 2 * meta.c0 + 1 : 2 * (meta.c0 + i)) * ROWS + r; };
-  float top = -INFINITY;
-  for (int i = lane; i < parts; i += 32) top = fmaxf(top, a.part_ml[index(i)].x);
-  top = warp_max(top);
-  const float ref = top == -INFINITY ? 0.f : top;
-  float sum = 0.f, o[E] = {};
-#pragma unroll 4
-  for (int i = 0; i < parts; ++i) {
-    const float2 ml = a.part_ml[index(i)];
-    const float f = exp2f(ml.x - ref);
-    sum = fmaf(ml.y, f, sum);
-    const float *src = a.part_o + index(i) * D + lane * E;
+  float top = -INFINITY, sum = 0.f, o[E] = {};
+#pragma unroll 1
+  for (int i0 = warp; i0 < parts; i0 += 4 * W) {
+    float2 ml[4];
+    float x[4][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(src[e], f, o[e]);
+    for (int j = 0; j < 4; ++j) {
+      const int i = i0 + j * W;
+      ml[j] = i < parts ? a.part_ml[index(i)] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[j][e] = i < parts ? a.part_o[index(i) * D + e * 32 + lane] : 0.f;
+    }
+    float now = top;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) now = fmaxf(now, ml[j].x);
+    const float ref = now == -INFINITY ? 0.f : now, f0 = exp2f(top - ref);
+    top = now;
+    sum *= f0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= f0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float f = exp2f(ml[j].x - ref);
+      sum = fmaf(ml[j].y, f, sum);
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = fmaf(x[j][e], f, o[e]);
+    }
   }
-  T *out = paged_out_row<T>(a, meta.b, h, row, D) + lane * E;
+  if (lane == 0) s_ml[warp] = make_float2(top, sum);
 #pragma unroll
-  for (int e = 0; e < E; ++e) out[e] = from_f32<T>(sum == 0.f ? 0.f : o[e] / sum);
-  if (lane == 0) paged_write_lse(a, meta.b, h, row, top, sum);
+  for (int e = 0; e < E; ++e) s_o[warp][e * 32 + lane] = o[e];
+  __syncthreads();
+  if (threadIdx.x >= D) return;
+  top = s_ml[0].x;
+#pragma unroll
+  for (int w = 1; w < W; ++w) top = fmaxf(top, s_ml[w].x);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float v = 0.f;
+  sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const float f = exp2f(s_ml[w].x - ref);
+    sum = fmaf(s_ml[w].y, f, sum);
+    v = fmaf(s_o[w][threadIdx.x], f, v);
+  }
+  paged_out_row<T>(a, meta.b, h, row, D)[threadIdx.x] = from_f32<T>(sum == 0.f ? 0.f : v / sum);
+  if (threadIdx.x == 0) paged_write_lse(a, meta.b, h, row, top, sum);
 }
 
 // w_out = w_in + sum over the rows of 2^(score - lse2): a thread a slot.

@@ -76,11 +76,12 @@ int paged_plan(PagedPlan *pl, const tsfm_kv_pages *p, int B, int M, int n_heads,
   // rows of a unit: fp32 what a thread's registers hold, bf16 16 to a warp
   int ctas = PA_F32_CTAS;
   if (p->dtype == TSFM_BF16) {
-    pl->rows = R <= 16 ? 16 : R <= 32 ? 32 : 64;
-    auto of = [&](auto one, auto two, auto four) { return R <= 16 ? decltype(one)::CTAS : R <= 32 ? decltype(two)::CTAS : decltype(four)::CTAS; };
-    ctas = p->d_head == 32   ? of(PagedMma<32, 1>(), PagedMma<32, 2>(), PagedMma<32, 4>())
-           : p->d_head == 64 ? of(PagedMma<64, 1>(), PagedMma<64, 2>(), PagedMma<64, 4>())
-                             : of(PagedMma<128, 1>(), PagedMma<128, 2>(), PagedMma<128, 4>());
+    pl->rows = R <= 8 ? 8 : R <= 16 ? 16 : R <= 32 ? 32 : 64;
+    auto of = [&](auto d) {
+      constexpr int D = decltype(d)::value;
+      return R <= 8 ? PagedMma<D, 1, 1>::CTAS : R <= 16 ? PagedMma<D, 2, 1>::CTAS : R <= 32 ? PagedMma<D, 2, 2>::CTAS : PagedMma<D, 2, 4>::CTAS;
+    };
+    ctas = p->d_head == 32 ? of(std::integral_constant<int, 32>()) : p->d_head == 64 ? of(std::integral_constant<int, 64>()) : of(std::integral_constant<int, 128>());
   } else {
     pl->rows = R == 1 ? 1 : R == 2 ? 2 : 4;
   }
@@ -99,17 +100,20 @@ int paged_plan(PagedPlan *pl, const tsfm_kv_pages *p, int B, int M, int n_heads,
   return TSFM_OK;
 }
 
-template <int D, int WR>
+template <int D, int NQ, int WR>
 cudaError_t launch_paged_mma(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl) {
-  using C = PagedMma<D, WR>;
+  using C = PagedMma<D, NQ, WR>;
   // (the attribute belongs to the device's context: set with every call, 0.2 us)
-  if (cudaError_t e = cudaFuncSetAttribute(paged_attn_mma_kernel<D, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES)) return e;
-  paged_attn_mma_kernel<D, WR><<<pl.grid, PA_THREADS, C::SMEM_BYTES, s>>>(a);
+  if (cudaError_t e = cudaFuncSetAttribute(paged_attn_mma_kernel<D, NQ, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES)) return e;
+  paged_attn_mma_kernel<D, NQ, WR><<<pl.grid, PA_MMA_THREADS, C::SMEM_BYTES, s>>>(a);
   return cudaGetLastError();
 }
 template <int D>
 cudaError_t launch_paged_rows(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl, bf16) {
-  return pl.rows == 16 ? launch_paged_mma<D, 1>(s, a, pl) : pl.rows == 32 ? launch_paged_mma<D, 2>(s, a, pl) : launch_paged_mma<D, 4>(s, a, pl);
+  return pl.rows == 8    ? launch_paged_mma<D, 1, 1>(s, a, pl)
+         : pl.rows == 16 ? launch_paged_mma<D, 2, 1>(s, a, pl)
+         : pl.rows == 32 ? launch_paged_mma<D, 2, 2>(s, a, pl)
+                         : launch_paged_mma<D, 2, 4>(s, a, pl);
 }
 template <int D>
 cudaError_t launch_paged_rows(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl, float) {
@@ -125,8 +129,10 @@ template <typename T, int D>
 cudaError_t launch_paged(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl) {
   if (cudaError_t e = launch_paged_rows<D>(s, a, pl, T())) return e;
   LAUNCHED();
-  if (pl.grid > 1) {
-    if (cudaError_t e = launch_after(s, dim3(pl.grid, (pl.rows + PA_JOIN_WARPS - 1) / PA_JOIN_WARPS), 32 * PA_JOIN_WARPS, paged_join_kernel<T, D>, a, pl.rows)) return e;
+  // nothing to join where no series has a second tile
+  if (a.pg.capacity > PA_TILE && pl.grid > 1) {
+    const unsigned rows = (unsigned)std::min<long long>(pl.rows, (long long)a.M * a.group);
+    if (cudaError_t e = launch_after(s, dim3(pl.grid, rows), 32 * PA_JOIN_WARPS, paged_join_kernel<T, D>, a, pl.rows)) return e;
     LAUNCHED();
   }
   if (a.w_out) {
