@@ -285,89 +285,124 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_f32_kernel(const __grid
 }
 
 // Joins the parts of the units that several CTAs shared: block x belongs to CTA x of the kernel before and works if that one is
-// the second of a unit's CTAs; block y is a row.  The warps share the parts: with one warp a row the 37 parts of
-// one series of 131071 slots (D 128) were a chain of loads as long as a third of the kernel before.
+// the second of a unit's CTAs; the y blocks share its rows.  Eight warps: each a row where a unit has few parts, all of them one
+// row where it has many (one series of 131071 slots has 37: a warp alone made them a chain of loads as long as a third of the
+// kernel before).
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * PA_JOIN_WARPS) paged_join_kernel(const __grid_constant__ PagedAttnArgs a, int ROWS) {
   constexpr int E = D / 32, W = PA_JOIN_WARPS;
   __shared__ float s_o[W][D];
   __shared__ float2 s_ml[W];
-  pdl_sync();
+  pdl_wait();
   const PagedMeta meta = a.meta[blockIdx.x];
   if (meta.b < 0 || meta.c0 + 1 != (int)blockIdx.x) return;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = blockIdx.y;
-  const int h = meta.u / a.chunks, row = (meta.u - h * a.chunks) * ROWS + r;
-  if (row >= a.M * a.group || row / a.group >= (a.n_new ? cut(a.n_new[meta.b], a.M) : a.M)) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int h = meta.u / a.chunks, row0 = (meta.u - h * a.chunks) * ROWS;
+  const int n_new = a.n_new ? cut(a.n_new[meta.b], a.M) : a.M;
+  const int rows = min(min(ROWS, a.M * a.group - row0), n_new * a.group - row0);       // live ones
   const int parts = meta.c1 - meta.c0 + 1;
-  auto index = [&](int i) { return (long long)(i == 0 ? 2 * meta.c0 + 1 : 2 * (meta.c0 + i)) * ROWS + r; };
-  float top = -INFINITY, sum = 0.f, o[E] = {};
+  const bool alone = parts <= 8;                   // a warp a row
+  const int share = alone ? 1 : W, sub = alone ? 0 : warp;
+  for (int r0 = blockIdx.y * (W / share); r0 < rows; r0 += gridDim.y * (W / share)) {
+    const int r = r0 + (alone ? warp : 0);
+    auto index = [&](int i) { return (long long)(i == 0 ? 2 * meta.c0 + 1 : 2 * (meta.c0 + i)) * ROWS + r; };
+    float top = -INFINITY, sum = 0.f, o[E] = {};
 #pragma unroll 1
-  for (int i0 = warp; i0 < parts; i0 += 4 * W) {
-    float2 ml[4];
-    float x[4][E];
+    for (int i0 = sub; i0 < parts && r < rows; i0 += 4 * share) {
+      float2 ml[4];
+      float x[4][E];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = i0 + j * W;
-      ml[j] = i < parts ? a.part_ml[index(i)] : make_float2(-INFINITY, 0.f);
+      for (int j = 0; j < 4; ++j) {
+        const int i = i0 + j * share;
+        ml[j] = i < parts ? a.part_ml[index(i)] : make_float2(-INFINITY, 0.f);
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[j][e] = i < parts ? a.part_o[index(i) * D + e * 32 + lane] : 0.f;
+        for (int e = 0; e < E; ++e) x[j][e] = i < parts ? a.part_o[index(i) * D + e * 32 + lane] : 0.f;
+      }
+      float now = top;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) now = fmaxf(now, ml[j].x);
+      const float ref = now == -INFINITY ? 0.f : now, f0 = exp2f(top - ref);
+      top = now;
+      sum *= f0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] *= f0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float f = exp2f(ml[j].x - ref);
+        sum = fmaf(ml[j].y, f, sum);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = fmaf(x[j][e], f, o[e]);
+      }
     }
-    float now = top;
+    if (!alone) {
+      __syncthreads();
+      if (lane == 0) s_ml[warp] = make_float2(top, sum);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) now = fmaxf(now, ml[j].x);
-    const float ref = now == -INFINITY ? 0.f : now, f0 = exp2f(top - ref);
-    top = now;
-    sum *= f0;
+      for (int e = 0; e < E; ++e) s_o[warp][e * 32 + lane] = o[e];
+      __syncthreads();
+      if (warp) continue;
+      top = s_ml[0].x;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] *= f0;
+      for (int w = 1; w < W; ++w) top = fmaxf(top, s_ml[w].x);
+      const float ref = top == -INFINITY ? 0.f : top;
+      sum = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float f = exp2f(ml[j].x - ref);
-      sum = fmaf(ml[j].y, f, sum);
+      for (int e = 0; e < E; ++e) o[e] = 0.f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = fmaf(x[j][e], f, o[e]);
+      for (int w = 0; w < W; ++w) {
+        const float f = exp2f(s_ml[w].x - ref);
+        sum = fmaf(s_ml[w].y, f, sum);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = fmaf(s_o[w][e * 32 + lane], f, o[e]);
+      }
     }
+    if (r >= rows) continue;
+    T *out = paged_out_row<T>(a, meta.b, h, row0 + r, D);
+#pragma unroll
+    for (int e = 0; e < E; ++e) out[e * 32 + lane] = from_f32<T>(sum == 0.f ? 0.f : o[e] / sum);
+    if (lane == 0) paged_write_lse(a, meta.b, h, row0 + r, top, sum);
   }
-  if (lane == 0) s_ml[warp] = make_float2(top, sum);
-#pragma unroll
-  for (int e = 0; e < E; ++e) s_o[warp][e * 32 + lane] = o[e];
-  __syncthreads();
-  if (threadIdx.x >= D) return;
-  top = s_ml[0].x;
-#pragma unroll
-  for (int w = 1; w < W; ++w) top = fmaxf(top, s_ml[w].x);
-  const float ref = top == -INFINITY ? 0.f : top;
-  float v = 0.f;
-  sum = 0.f;
-#pragma unroll
-  for (int w = 0; w < W; ++w) {
-    const float f = exp2f(s_ml[w].x - ref);
-    sum = fmaf(s_ml[w].y, f, sum);
-    v = fmaf(s_o[w][threadIdx.x], f, v);
-  }
-  paged_out_row<T>(a, meta.b, h, row, D)[threadIdx.x] = from_f32<T>(sum == 0.f ? 0.f : v / sum);
-  if (threadIdx.x == 0) paged_write_lse(a, meta.b, h, row, top, sum);
+  pdl_release();
 }
 
-// w_out = w_in + sum over the rows of 2^(score - lse2): a thread a slot.
-__global__ void __launch_bounds__(256) paged_weights_kernel(const __grid_constant__ PagedAttnArgs a) {
+// w_out = w_in + sum over the rows of 2^(score - lse2); a slot that a row does not see has the score -inf there.  A thread four
+// slots, eight rows of scores in flight.
+constexpr int PA_WEIGHT_ROWS = 64;
+__global__ void __launch_bounds__(128) paged_weights_kernel(const __grid_constant__ PagedAttnArgs a) {
+  __shared__ float s_lse[PA_WEIGHT_ROWS];
   pdl_wait();
   const int Hkv = a.pg.n_kv_heads, b = blockIdx.x / Hkv, R = a.M * a.group;
   const PagedSpan s = paged_span(a, b, false);
   const float *w_in = a.w_in ? a.w_in + blockIdx.x * a.w_stride : nullptr;
   float *w_out = a.w_out + blockIdx.x * a.w_stride;
-  for (int slot = blockIdx.y * 256 + threadIdx.x; slot < s.total; slot += gridDim.y * 256) {
-    float w = w_in ? w_in[slot] : 0.f;
-    for (int m = 0; m < s.n_new; ++m) {
-      const int2 range = paged_row_range(a, s, m);
-      if (slot < range.x || slot >= range.y) continue;
-      for (int g = 0; g < a.group; ++g) {
-        const long long row = (long long)blockIdx.x * R + m * a.group + g;
-        const float lse2 = a.lse2[row];
-        if (lse2 != -INFINITY) w += exp2f(a.scores[row * a.score_stride + slot] - lse2);
+  const int live = s.n_new * a.group;
+  for (int base = blockIdx.y * 512; base < s.total; base += gridDim.y * 512) {
+    const int slot = base + threadIdx.x * 4;
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int r0 = 0; r0 < live; r0 += PA_WEIGHT_ROWS) {
+      __syncthreads();
+      if (threadIdx.x < PA_WEIGHT_ROWS) {          // (a row that got nothing gives nothing)
+        const float lse2 = r0 + threadIdx.x < live ? a.lse2[(long long)blockIdx.x * R + r0 + threadIdx.x] : INFINITY;
+        s_lse[threadIdx.x] = lse2 == -INFINITY ? INFINITY : lse2;
+      }
+      __syncthreads();
+      if (slot >= s.total || slot < s.tile0 * PA_TILE) continue;       // before the first tile nothing was seen
+      const float *src = a.scores + ((long long)blockIdx.x * R + r0) * a.score_stride + slot;
+      const int n = min(PA_WEIGHT_ROWS, live - r0);
+      for (int r = 0; r < n; r += 8) {
+        float4 v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = r + j < n ? *reinterpret_cast<const float4 *>(src + (r + j) * a.score_stride) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float lse2 = r + j < n ? s_lse[r + j] : INFINITY;
+          w[0] += exp2f(v[j].x - lse2), w[1] += exp2f(v[j].y - lse2), w[2] += exp2f(v[j].z - lse2), w[3] += exp2f(v[j].w - lse2);
+        }
       }
     }
-    w_out[slot] = w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (slot + e < s.total) w_out[slot + e] = (w_in ? w_in[slot + e] : 0.f) + w[e];
   }
 }
 

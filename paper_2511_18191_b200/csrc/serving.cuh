@@ -131,13 +131,13 @@ cudaError_t launch_paged(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan
   LAUNCHED();
   // nothing to join where no series has a second tile
   if (a.pg.capacity > PA_TILE && pl.grid > 1) {
-    const unsigned rows = (unsigned)std::min<long long>(pl.rows, (long long)a.M * a.group);
+    const unsigned rows = (unsigned)std::min<long long>(8, std::min<long long>(pl.rows, (long long)a.M * a.group));
     if (cudaError_t e = launch_after(s, dim3(pl.grid, rows), 32 * PA_JOIN_WARPS, paged_join_kernel<T, D>, a, pl.rows)) return e;
     LAUNCHED();
   }
   if (a.w_out) {
-    const long long chunks = (a.pg.capacity + 255ll) / 256;
-    if (cudaError_t e = launch_after(s, dim3((unsigned)(a.B * a.pg.n_kv_heads), (unsigned)std::min(chunks, 4096ll)), 256, paged_weights_kernel, a)) return e;
+    const long long chunks = (a.pg.capacity + 511ll) / 512;
+    if (cudaError_t e = launch_after(s, dim3((unsigned)(a.B * a.pg.n_kv_heads), (unsigned)std::min(chunks, 4096ll)), 128, paged_weights_kernel, a)) return e;
     LAUNCHED();
   }
   return cudaSuccess;
