@@ -21,7 +21,7 @@ TSFM_DRAFT_SEPARATE, TSFM_DRAFT_LAYER_SKIP = 0, 1
 TSFM_GEMM_AUTO, TSFM_GEMM_SIMT, TSFM_GEMM_WS = 0, 1, 2
 TSFM_EXEC_GRAPH, TSFM_EXEC_STREAM, TSFM_EXEC_NO_PDL, TSFM_EXEC_NO_COMPACT, TSFM_EXEC_CHECK_BOUNDS = 0, 1, 2, 4, 8
 TSFM_MAX_K = 32
-TSFM_PAGES_BAD_ID, TSFM_PAGES_BAD_LEN = 1, 2
+TSFM_PAGES_BAD_ID, TSFM_PAGES_BAD_LEN, TSFM_PAGES_TIMEOUT = 1, 2, 4
 TSFM_ROPE_HALF, TSFM_ROPE_INTERLEAVED = 0, 1
 TSFM_ROPE_PLAIN, TSFM_ROPE_LINEAR, TSFM_ROPE_BASE, TSFM_ROPE_PARTS = 0, 1, 2, 3
 

@@ -27,6 +27,7 @@ struct PagedAttnArgs {
   long long q_stride, out_stride;                  // elements
   const int *len, *n_new;                          // n_new or NULL
   int B, M, n_heads, group;                        // group = n_heads / n_kv_heads
+  uint32_t group_magic;                            // ceil(2^32 / group): see token_of
   float scale2;                                    // scale * log2(e)
   int causal, window;
   float *lse;                                      // or NULL
@@ -42,15 +43,17 @@ struct PagedAttnArgs {
   long long score_stride;
 };
 
+// The token of a query row (row / group).  Rows and groups are below 2^16, so the rounded-up reciprocal is exact.
+__device__ __forceinline__ int token_of(const PagedAttnArgs &a, int row) { return a.group == 1 ? row : (int)__umulhi((uint32_t)row, a.group_magic); }
+
 // A series as this call sees it: its live rows, the slots that any of them sees, the tiles that hold those.
 struct PagedSpan {
   int len, n_new, total, lo, tile0, tiles;
 };
-__device__ __forceinline__ PagedSpan paged_span(const PagedAttnArgs &a, int b, bool report) {
+__device__ __forceinline__ PagedSpan paged_span_of(const PagedAttnArgs &a, int raw, int raw_new, bool report) {
   PagedSpan s;
-  const int raw = __ldg(a.len + b);
   s.len = cut(raw, a.pg.capacity);
-  s.n_new = a.n_new ? cut(__ldg(a.n_new + b), a.M) : a.M;
+  s.n_new = cut(raw_new, a.M);
   const long long total = (long long)s.len + (a.causal ? s.n_new : 0);
   s.total = (int)min(total, (long long)a.pg.capacity);
   if (report && (raw != s.len || total != s.total)) pages_report(a.pg, BAD_LEN);
@@ -60,6 +63,9 @@ __device__ __forceinline__ PagedSpan paged_span(const PagedAttnArgs &a, int b, b
   // a live row without slots still has an answer: one tile
   s.tiles = s.n_new == 0 ? 0 : max(1, (s.total + PA_TILE - 1) / PA_TILE - s.tile0);
   return s;
+}
+__device__ __forceinline__ PagedSpan paged_span(const PagedAttnArgs &a, int b, bool report) {
+  return paged_span_of(a, __ldg(a.len + b), a.n_new ? __ldg(a.n_new + b) : a.M, report);
 }
 // Slots [lo, end) that row m sees.
 __device__ __forceinline__ int2 paged_row_range(const PagedAttnArgs &a, const PagedSpan &s, int m) {
@@ -115,14 +121,14 @@ __device__ PagedRun paged_find_run(const PagedAttnArgs &a) {
 
 // Where a row's result goes: straight to the caller, or as a part into the workspace.
 __device__ __forceinline__ void paged_write_lse(const PagedAttnArgs &a, int b, int h, int row, float m, float l) {
-  const int tok = row / a.group, head = h * a.group + row - tok * a.group;
+  const int tok = token_of(a, row), head = h * a.group + row - tok * a.group;
   const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
   if (a.lse) a.lse[((long long)b * a.M + tok) * a.n_heads + head] = lse2 * 0.69314718055994530942f;
   if (a.lse2) a.lse2[((long long)b * a.pg.n_kv_heads + h) * a.M * a.group + row] = lse2;
 }
 template <typename T>
 __device__ __forceinline__ T *paged_out_row(const PagedAttnArgs &a, int b, int h, int row, int D) {
-  const int tok = row / a.group, head = h * a.group + row - tok * a.group;
+  const int tok = token_of(a, row), head = h * a.group + row - tok * a.group;
   return reinterpret_cast<T *>(a.out) + ((long long)b * a.M + tok) * a.out_stride + (long long)head * D;
 }
 
@@ -136,6 +142,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_f32_kernel(const __grid
   __shared__ float2 s_ml[WARPS][ROWS];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l8 = lane & 7, grp = lane >> 3;
   PagedRun run = paged_find_run<PA_THREADS>(a);
+  pdl_release();
   if (threadIdx.x == 0) {
     PagedMeta meta{-1, 0, 0, 0};
     if (run.count > 0 && run.first) {
@@ -159,8 +166,8 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_f32_kernel(const __grid
     for (int r = 0; r < ROWS; ++r) {
       m[r] = -INFINITY;
       l[r] = 0.f;
-      range[r] = r < rows ? paged_row_range(a, s, (row0 + r) / a.group) : make_int2(0, 0);
-      const int tok = r < rows ? (row0 + r) / a.group : 0, head = h * a.group + (r < rows ? row0 + r - tok * a.group : 0);
+      range[r] = r < rows ? paged_row_range(a, s, token_of(a, row0 + r)) : make_int2(0, 0);
+      const int tok = r < rows ? token_of(a, row0 + r) : 0, head = h * a.group + (r < rows ? row0 + r - tok * a.group : 0);
       const float *src = reinterpret_cast<const float *>(a.q) + ((long long)run.b * a.M + tok) * a.q_stride + (long long)head * D;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
@@ -268,7 +275,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attn_f32_kernel(const __grid
         v = fmaf(s_o[w][r][d], f, v);
       }
       if (whole) {
-        if ((row0 + r) / a.group < s.n_new) {
+        if (token_of(a, row0 + r) < s.n_new) {
           paged_out_row<float>(a, run.b, h, row0 + r, D)[d] = sum == 0.f ? 0.f : v / sum;
           if (d == 0) paged_write_lse(a, run.b, h, row0 + r, top, sum);
         }
@@ -293,7 +300,7 @@ __global__ void __launch_bounds__(32 * PA_JOIN_WARPS) paged_join_kernel(const __
   constexpr int E = D / 32, W = PA_JOIN_WARPS;
   __shared__ float s_o[W][D];
   __shared__ float2 s_ml[W];
-  pdl_wait();
+  pdl_sync();
   const PagedMeta meta = a.meta[blockIdx.x];
   if (meta.b < 0 || meta.c0 + 1 != (int)blockIdx.x) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -362,7 +369,6 @@ __global__ void __launch_bounds__(32 * PA_JOIN_WARPS) paged_join_kernel(const __
     for (int e = 0; e < E; ++e) out[e * 32 + lane] = from_f32<T>(sum == 0.f ? 0.f : o[e] / sum);
     if (lane == 0) paged_write_lse(a, meta.b, h, row0 + r, top, sum);
   }
-  pdl_release();
 }
 
 // w_out = w_in + sum over the rows of 2^(score - lse2); a slot that a row does not see has the score -inf there.  A thread four

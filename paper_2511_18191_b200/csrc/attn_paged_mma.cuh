@@ -4,54 +4,82 @@
 // WR x WK warps compute: a warp takes 8 NQ query rows against 64 / WK of a tile's slots, with a running maximum and sum of its own;
 // the WK warps of a row are merged when the unit ends.  Slots are the M side of the products and queries the N side (S^T = K Q^T,
 // O^T = V^T P^T, P^T by one 8 x 8 transposition per eight slots): rows come in eights, not sixteens, and eight cost half of the
-// instructions and registers.  A fifth warp fetches: it looks the pages up, a slot a lane, and brings tiles (and the queries of a
-// unit's first one) in by cp.async, up to STAGES - 1 ahead and across unit borders; slots that no row sees arrive as zeros.  Named
-// barriers hand the stages over.  Precision: scores of bf16 operands in fp32; probabilities as two bf16 parts, so that only the
+// instructions and registers.  One more warp fetches: a TMA copy of up to 64 slots of
+// a page, head and 64 elements (pages of less than eight slots, and pools that TMA has no map for: cp.async, a slot's row at a
+// time), and the queries of a unit's first tile, up to STAGES - 1 tiles ahead and across unit borders.  It alone waits for copies;
+// named barriers hand the stages over.  Precision: scores of bf16 operands in fp32; probabilities as two bf16 parts, so that only the
 // result is rounded.
 #pragma once
 #include "attn_narrow.cuh"
 #include "attn_paged.cuh"
+#include "gemm_tc.cuh"
 
 namespace tsfm {
 
-template <int D, int NQ, int WR> struct PagedMma {
-  static constexpr int WK = 4 / WR, KEYS = PA_TILE / WK, BLOCKS = KEYS / 16;
+template <int D_, int NQ_, int WR_> struct PagedMma {
+  static constexpr int D = D_, NQ = NQ_, WR = WR_;
+  static constexpr int WK = 2, KEYS = PA_TILE / WK, BLOCKS = KEYS / 16;
+  static constexpr int WARPS = WR * WK, THREADS = 32 * WARPS + 32;
   static constexpr int WROWS = 8 * NQ, ROWS = WROWS * WR, RB = D * 2;
+  // keys and values of a stage: parts of 64 (32) elements, [part][slot], 16-byte chunks exchanged as TMA's 128-byte (64-byte)
+  // swizzle does, which is flash_swz of such rows
+  static constexpr int PD = D < 64 ? D : 64, PARTS = D / PD, PB = PD * 2, PART_BYTES = PA_TILE * PB;
   static constexpr int KV_BYTES = PA_TILE * RB, Q_BYTES = ROWS * RB;
-  // the merge, through one stage: rows of D + 4 floats (lanes of a store then meet different banks), maximum and sum
-  static constexpr int MERGE_ROW = D + 4, MERGE_BYTES = 4 * WROWS * (MERGE_ROW * 4 + 8);
-  static constexpr int STAGE_BYTES = ((2 * KV_BYTES + Q_BYTES > MERGE_BYTES ? 2 * KV_BYTES + Q_BYTES : MERGE_BYTES) + 255) / 256 * 256;
-  static constexpr int STAGES = D == 128 ? (WR == 1 ? 3 : 2) : D == 64 ? (WR == 1 ? 4 : 3) : 4;
-  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES;
+  // the merge, through one stage: a lane's float4s
+  static constexpr int MERGE_WORDS = NQ + NQ * D / 16;
+  static constexpr int STAGE_BYTES = (2 * KV_BYTES + Q_BYTES + 1023) / 1024 * 1024;
+  static_assert(WR * (WK - 1) * 32 * MERGE_WORDS * 16 <= STAGE_BYTES, "the merge takes one stage");
+  static constexpr int STAGES = 3;
+  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + 1024;        // (stages begin at multiples of 1 KB)
   // resident CTAs on an SM: beside the stages what describes them, the scan (128 bytes), alignment, and 1 KB that a CTA costs
-  static constexpr int BY_SMEM = 228 * 1024 / (SMEM_BYTES + STAGES * 24 + 128 + 256 + 1024);
-  static constexpr int CTAS = BY_SMEM < 4 ? BY_SMEM : 4;
+  static constexpr int BY_SMEM = 228 * 1024 / (SMEM_BYTES + STAGES * 128 + 128 + 1024);
+  static constexpr int CTAS = D == 128 ? (BY_SMEM < 2 ? BY_SMEM : 2) : BY_SMEM < 4 ? BY_SMEM : 4;
 };
-
-constexpr int PA_MMA_THREADS = PA_THREADS + 32;
 
 // Barriers between the fetching warp and the others: `full` of a stage, `empty` of a stage; and one among the others.
 __device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ void bar_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
-// A tile in a stage: unit u of series b, its t-th tile.
+// A tile on its way: unit u of series b, its t-th tile, and the series' span.  first: the unit's queries come with it.
 struct PagedItem {
-  int b, u, t, first;                              // first: its queries come with it
+  int b, u, t, first;
+  PagedSpan sp;
 };
 
-template <int D, int NQ, int WR>
-__global__ void __launch_bounds__(PA_MMA_THREADS, PagedMma<D, NQ, WR>::CTAS) paged_attn_mma_kernel(const __grid_constant__ PagedAttnArgs a) {
-  using C = PagedMma<D, NQ, WR>;
+// TMA tile of a page's slots: {first element, slot, head, page}.
+__device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap *map, int x, int slot, int head, int page, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(map), "r"(x), "r"(slot), "r"(head), "r"(page), "r"(bar) : "memory");
+}
+// Bounded wait for a tile: false if it did not arrive within TC_WAIT_NS.
+__device__ __forceinline__ bool tile_arrived(uint32_t bar, uint32_t parity) {
+  unsigned long long t0 = 0;
+  for (uint32_t n = 0;; ++n) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if (n == 256) t0 = globaltimer_ns();
+    if (n > 256 && (n & 255) == 0 && globaltimer_ns() - t0 > TC_WAIT_NS) return false;
+  }
+}
+
+template <typename C, bool TMA>
+__global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_mma_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV) {
+  constexpr int D = C::D, NQ = C::NQ;
   constexpr int WK = C::WK, KEYS = C::KEYS, NB = C::BLOCKS, ROWS = C::ROWS, WROWS = C::WROWS, RB = C::RB, S = C::STAGES;
   constexpr int FULL = 1, EMPTY = 1 + S, MERGE = 1 + 2 * S;
-  extern __shared__ __align__(256) unsigned char paged_smem[];
+  constexpr int PD = C::PD, PB = C::PB, PARTS = C::PARTS;
+  extern __shared__ __align__(1024) unsigned char paged_smem_raw[];
+  __shared__ alignas(8) unsigned long long s_full[S];                  // TMA's barriers, waited on by the fetching warp alone
   __shared__ unsigned s_valid[S][2];               // slots of the tile that exist: in [lo, total), page in the pool
-  __shared__ PagedItem s_item[S];
+  __shared__ PagedItem s_item[S], s_next[S];       // of the stages; of the tiles whose page ids are on their way
+  __shared__ int s_ids[S][TMA ? 8 : PA_TILE];      // those ids
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wr = warp / WK, wk = warp % WK;
   const int g = lane >> 2, t4 = lane & 3;
-  const uint32_t smem0 = (uint32_t)__cvta_generic_to_shared(paged_smem);
+  const uint32_t smem0 = (smem_u32(paged_smem_raw) + 1023u) & ~1023u;
+  unsigned char *const paged_smem = paged_smem_raw + (smem0 - smem_u32(paged_smem_raw));
   const int R = a.M * a.group;
-  const PagedRun run = paged_find_run<PA_MMA_THREADS>(a);
+  const PagedRun run = paged_find_run<C::THREADS>(a);
+  pdl_release();                                   // (the join waits for this grid's end; its CTAs may take their places)
   if (tid == 0) {
     PagedMeta meta{-1, 0, 0, 0};
     if (run.count > 0 && run.first) {
@@ -62,82 +90,157 @@ __global__ void __launch_bounds__(PA_MMA_THREADS, PagedMma<D, NQ, WR>::CTAS) pag
   }
   if (run.count == 0) return;
 
-  if (warp == PA_THREADS / 32) {
+  if (warp == C::WARPS) {
     constexpr int CPR = D / 8, STEP = 32 / CPR;    // 16-byte chunks of a row; rows of a copy instruction
     const int chunk = lane % CPR, sub = lane / CPR;
-    int b = run.b, u = run.u, t = run.first;
+    // Page ids travel like the tiles, AHEAD tiles before theirs and in the same groups: a plain load behind the queue of copies
+    // returned after 6000 to 17000 cycles and stood between each tile and the next.
+    constexpr int AHEAD = S - 1;
+    int b = run.b, u = run.u, t = run.first, ni = 0;
     PagedSpan sp = paged_span(a, b, false);
-    long long off[2];                              // byte offsets of slots lane, lane + 32 of the next tile; -1: hidden
-    auto look_up = [&]() {
+    int len_next = 0, new_next = 0;                // of series b + 1, looked at when it is reached
+    auto fetch_next = [&]() {
+      const int at = min(b + 1, a.B - 1);
+      len_next = __ldg(a.len + at);
+      new_next = a.n_new ? __ldg(a.n_new + at) : a.M;
+    };
+    fetch_next();
+    // TMA copies boxes of up to 64 slots of one page: a page id a box, else a slot
+    const int box_log = TMA ? min(a.pg.page_log, 6) : 0, boxes = PA_TILE >> box_log;
+    const uint32_t full0 = smem_u32(s_full);
+    bool dead = false;                             // a tile did not arrive: nothing more is fetched or waited for
+    if (TMA) {
+      if (lane < S) mbar_init(full0 + 8 * lane, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+    }
+    auto fetch_ids = [&]() {                       // of tile ni; then moves on
+      if (ni >= run.count) return;
+      const int ring = ni % S;
       const int *row = a.pg.table + (long long)b * a.pg.table_stride;
-      int page[2];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int slot = (sp.tile0 + t) * PA_TILE + 32 * x + lane;
-        page[x] = slot >= sp.lo && slot < sp.total ? page_of(a.pg, row, slot) : -2;
+      for (int x = 0; x < (TMA ? 1 : 2); ++x) {
+        const int j = 32 * x + lane, slot = (sp.tile0 + t) * PA_TILE + (j << box_log);
+        if (j < boxes && slot + (1 << box_log) > sp.lo && slot < sp.total)
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(&s_ids[ring][j])), "l"(row + (slot >> a.pg.page_log)) : "memory");
       }
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        off[x] = page[x] < 0 ? -1 : slot_offset(a.pg, page[x], u / a.chunks, (sp.tile0 + t) * PA_TILE + 32 * x + lane);
-        if (page[x] == -1) pages_report(a.pg, BAD_ID);
+      if (lane == 0) s_next[ring] = PagedItem{b, u, t, ni == 0 || t == 0, sp};
+      if (++ni == run.count) return;
+      if (++t == sp.tiles) {
+        t = 0;
+        if (++u == a.units) {
+          u = 0;
+          do {                                     // (there is one: the run goes on)
+            ++b;
+            sp = paged_span_of(a, len_next, new_next, false);
+            fetch_next();
+          } while (sp.tiles == 0);
+        }
       }
     };
-    look_up();
+    for (int j = 0; j < AHEAD; ++j) fetch_ids();
+    flash_commit();
+    flash_wait<0>();
     int stage = 0;
     for (int i = 0; i < run.count; ++i) {
       const uint32_t dst = smem0 + stage * C::STAGE_BYTES;
-      if (i >= S) bar_sync(EMPTY + stage, PA_MMA_THREADS);
-      const unsigned v0 = __ballot_sync(0xffffffffu, off[0] >= 0), v1 = __ballot_sync(0xffffffffu, off[1] >= 0);
-      const bool first = i == 0 || t == 0;
-      if (lane == 0) {
-        s_valid[stage][0] = v0, s_valid[stage][1] = v1;
-        s_item[stage] = PagedItem{b, u, t, first};
-      }
+      __syncwarp();
+      const PagedItem it = s_next[stage];
+      const int h = it.u / a.chunks;
+      const int base = (it.sp.tile0 + it.t) * PA_TILE;
+      long long off[2] = {-1, -1};                 // (plain copies) byte offsets of slots lane, lane + 32; -1: hidden
+      int page = -1;                               // (TMA) of box lane % 8
+      unsigned v[2];
+      if (TMA) {
+        const int j = lane & 7, slot = base + (j << box_log);
+        if (j < boxes && slot + (1 << box_log) > it.sp.lo && slot < it.sp.total) {
+          page = s_ids[stage][j];
+          if ((unsigned)page >= (unsigned)a.pg.n_pages) {
+            page = -1;
+            pages_report(a.pg, BAD_ID);
+          }
+        }
+        const unsigned ok = __ballot_sync(0xffffffffu, page >= 0) & 0xff;
 #pragma unroll
-      for (int r = 0; r < PA_TILE; r += STEP) {
-        const long long o = __shfl_sync(0xffffffffu, off[r / 32], (r & 31) + sub);
-        const uint32_t at = dst + (r + sub) * RB + flash_swz<D>(r + sub, chunk) * 16;
-        const long long from = (o < 0 ? 0 : o) + chunk * 16;
-        const int bytes = o < 0 ? 0 : 16;
-        asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(at), "l"(a.pg.k + from), "r"(bytes) : "memory");
-        asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(at + C::KV_BYTES), "l"(a.pg.v + from), "r"(bytes) : "memory");
+        for (int x = 0; x < 2; ++x) {
+          const int at = 32 * x + lane;
+          v[x] = __ballot_sync(0xffffffffu, base + at >= it.sp.lo && base + at < it.sp.total && (ok >> (at >> box_log) & 1));
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int slot = base + 32 * x + lane;
+          if (slot >= it.sp.lo && slot < it.sp.total) {
+            const int id = s_ids[stage][32 * x + lane];
+            if ((unsigned)id < (unsigned)a.pg.n_pages) off[x] = slot_offset(a.pg, id, h, slot);
+            else pages_report(a.pg, BAD_ID);
+          }
+          v[x] = __ballot_sync(0xffffffffu, off[x] >= 0);
+        }
       }
-      if (first) {
-        const int h = u / a.chunks, row0 = (u - h * a.chunks) * ROWS;
+      __syncwarp();
+      fetch_ids();
+      if (i >= S) bar_sync(EMPTY + stage, C::THREADS);
+      if (lane == 0) {
+        s_valid[stage][0] = v[0], s_valid[stage][1] = v[1];
+        s_item[stage] = it;
+      }
+      if (TMA) {
+        const int part = (lane >> 3) % PARTS, kv = (lane >> 3) / PARTS;
+        const unsigned ok = __ballot_sync(0xffffffffu, page >= 0) & 0xff;
+        if (lane == 0 && !dead) mbar_expect_tx(full0 + 8 * stage, __popc(ok) * 2 * PARTS * (PB << box_log));
+        __syncwarp();
+        if (page >= 0 && kv < 2 && !dead) {
+          const int slot = base + ((lane & 7) << box_log);
+          tma_load_page(dst + kv * C::KV_BYTES + part * C::PART_BYTES + ((lane & 7) << box_log) * PB, kv ? &mapV : &mapK, part * PD,
+                        slot & ((1 << a.pg.page_log) - 1), h, page, full0 + 8 * stage);
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < PA_TILE; r += STEP) {
+          const long long o = __shfl_sync(0xffffffffu, off[r / 32], (r & 31) + sub);
+          const uint32_t at = dst + (chunk / (PD / 8)) * C::PART_BYTES + (r + sub) * PB + flash_swz<PD>(r + sub, chunk % (PD / 8)) * 16;
+          const long long from = (o < 0 ? 0 : o) + chunk * 16;
+          const int bytes = o < 0 ? 0 : 16;        // hidden slots arrive as zeros
+          asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(at), "l"(a.pg.k + from), "r"(bytes) : "memory");
+          asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(at + C::KV_BYTES), "l"(a.pg.v + from), "r"(bytes) : "memory");
+        }
+      }
+      if (it.first) {
+        const int row0 = (it.u - h * a.chunks) * ROWS;
 #pragma unroll 4
         for (int r = sub; r < ROWS; r += STEP) {
           const bool in = row0 + r < R;
-          const int tok = in ? (row0 + r) / a.group : 0, head = h * a.group + (in ? row0 + r - tok * a.group : 0);
-          const bf16 *src = reinterpret_cast<const bf16 *>(a.q) + ((long long)b * a.M + tok) * a.q_stride + (long long)head * D + chunk * 8;
+          const int tok = in ? token_of(a, row0 + r) : 0, head = h * a.group + (in ? row0 + r - tok * a.group : 0);
+          const bf16 *src = reinterpret_cast<const bf16 *>(a.q) + ((long long)it.b * a.M + tok) * a.q_stride + (long long)head * D + chunk * 8;
           const uint32_t at = dst + 2 * C::KV_BYTES + r * RB + flash_swz<D>(r, chunk) * 16;
           asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(src), "r"(in ? 16 : 0) : "memory");
         }
       }
       flash_commit();
-      if (i + 1 < run.count) {
-        if (++t == sp.tiles) {
-          t = 0;
-          if (++u == a.units) {
-            u = 0;
-            do sp = paged_span(a, ++b, false); while (sp.tiles == 0);        // (there is one: the run goes on)
-          }
+      auto hand_over = [&](int tile) {
+        if (TMA && !dead && __any_sync(0xffffffffu, !tile_arrived(full0 + 8 * (tile % S), (tile / S) & 1))) {
+          dead = true;
+          pages_report(a.pg, PAGES_TIMEOUT);
         }
-        look_up();
-      }
+        __threadfence_block();
+        bar_arrive(FULL + tile % S, C::THREADS);
+      };
       if (i >= S - 2) {
         flash_wait<S - 2>();
-        __threadfence_block();
-        bar_arrive(FULL + (stage + 2) % S, PA_MMA_THREADS);                   // tile i - (S - 2)
+        hand_over(i - (S - 2));
+      }
+      if (i + 1 == run.count) {
+        flash_wait<0>();
+        for (int tile = max(0, run.count - (S - 2)); tile < run.count; ++tile) hand_over(tile);
       }
       if (++stage == S) stage = 0;
     }
-    flash_wait<0>();
-    __threadfence_block();
-    for (int i = max(0, run.count - (S - 2)); i < run.count; ++i) bar_arrive(FULL + i % S, PA_MMA_THREADS);
     return;
   }
 
-  const FlashLane<D> fl(lane);
+  const FlashLane<PD> fl(lane);
   const uint32_t key_at = fl.va, value_at = fl.ka;  // (keys are the M side here: rows and chunks change places)
   uint32_t qf[NQ][D / 16][2];
   float o[NQ][D / 16][4], m[NQ][2], l[NQ][2];      // of queries 2 t4, 2 t4 + 1 of each tile of eight; l of this lane's slots only
@@ -146,11 +249,11 @@ __global__ void __launch_bounds__(PA_MMA_THREADS, PagedMma<D, NQ, WR>::CTAS) pag
   int stage = 0;
 #pragma unroll 1
   for (int i = 0; i < run.count; ++i) {
-    bar_sync(FULL + stage, PA_MMA_THREADS);
+    bar_sync(FULL + stage, C::THREADS);
     const PagedItem it = s_item[stage];
     const uint32_t kst = smem0 + stage * C::STAGE_BYTES, vst = kst + C::KV_BYTES;
     if (it.first) {
-      const PagedSpan s = paged_span(a, it.b, false);
+      const PagedSpan s = it.sp;
       h = it.u / a.chunks, row0 = (it.u - h * a.chunks) * ROWS;
       total = s.total, tile0 = s.tile0, tiles = s.tiles, len_lo = s.lo, n_new = s.n_new, seg_first = it.t;
 #pragma unroll
@@ -158,12 +261,12 @@ __global__ void __launch_bounds__(PA_MMA_THREADS, PagedMma<D, NQ, WR>::CTAS) pag
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const int row = row0 + wr * WROWS + q * 8 + t4 * 2 + x;
-          range[q][x] = row < R ? paged_row_range(a, s, row / a.group) : make_int2(0, 0);
+          range[q][x] = row < R ? paged_row_range(a, s, token_of(a, row)) : make_int2(0, 0);
           m[q][x] = -INFINITY;
           l[q][x] = 0.f;
         }
-      min_end = paged_row_range(a, s, row0 / a.group).y;
-      max_start = paged_row_range(a, s, min(s.n_new, (min(R, row0 + ROWS) - 1) / a.group + 1) - 1).x;
+      min_end = paged_row_range(a, s, token_of(a, row0)).y;
+      max_start = paged_row_range(a, s, min(s.n_new, token_of(a, min(R, row0 + ROWS) - 1) + 1) - 1).x;
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
         const int qrow = wr * WROWS + q * 8 + (lane & 7);
@@ -183,26 +286,30 @@ __global__ void __launch_bounds__(PA_MMA_THREADS, PagedMma<D, NQ, WR>::CTAS) pag
 
     // scores, slots x queries
     float s[NB][NQ][4];
-    const uint32_t ka = kst + wk * KEYS * RB + key_at;
+    const uint32_t ka = kst + wk * KEYS * PB + key_at;
+    {
+      // (two sums each where a warp has few of them: a product waits some 35 cycles for the one before)
+      constexpr int CH = NB * NQ < 4 ? 2 : 1;
+      float c[CH][NB][NQ][4];
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
+      for (int i = 0; i < CH * NB * NQ * 4; ++i) (&c[0][0][0][0])[i] = 0.f;
 #pragma unroll
-      for (int q = 0; q < NQ; ++q) s[n][q][0] = s[n][q][1] = s[n][q][2] = s[n][q][3] = 0.f;
+      for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        uint32_t k[4];
-        flash_ldsm4((ka + n * 16 * RB) ^ (uint32_t)(ks * 32), k);
+        for (int n = 0; n < NB; ++n) {
+          uint32_t k[4];
+          flash_ldsm4((ka + n * 16 * PB + ks / (PD / 16) * C::PART_BYTES) ^ (uint32_t)(ks % (PD / 16) * 32), k);
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) mma_bf16_16816(s[n][q], k, qf[q][ks][0], qf[q][ks][1]);
-      }
+          for (int q = 0; q < NQ; ++q) mma_bf16_16816(c[ks % CH][n][q], k, qf[q][ks][0], qf[q][ks][1]);
+        }
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int q = 0; q < NQ; ++q)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) s[n][q][x] = (CH == 2 ? c[0][n][q][x] + c[CH - 1][n][q][x] : c[0][n][q][x]) * a.scale2;
     }
     const bool open = valid == ~0ull && base >= max_start && base + PA_TILE <= min_end;      // every row sees every slot
-#pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-      for (int q = 0; q < NQ; ++q)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) s[n][q][x] *= a.scale2;
     if (!open) {
 #pragma unroll
       for (int n = 0; n < NB; ++n)
@@ -231,9 +338,10 @@ __global__ void __launch_bounds__(PA_MMA_THREADS, PagedMma<D, NQ, WR>::CTAS) pag
         }
     }
     // running softmax
+    float alpha[NQ][2];
+    bool moved = false;
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-      float alpha[2];
+    for (int q = 0; q < NQ; ++q)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         float top = m[q][x];
@@ -243,7 +351,8 @@ __global__ void __launch_bounds__(PA_MMA_THREADS, PagedMma<D, NQ, WR>::CTAS) pag
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
         const float ref = top == -INFINITY ? 0.f : top;
-        alpha[x] = flash_ex2(m[q][x] - ref);
+        alpha[q][x] = flash_ex2(m[q][x] - ref);
+        moved |= alpha[q][x] != 1.f;
         m[q][x] = top;
         float sum = 0.f;
 #pragma unroll
@@ -252,24 +361,34 @@ __global__ void __launch_bounds__(PA_MMA_THREADS, PagedMma<D, NQ, WR>::CTAS) pag
           s[n][q][2 + x] = flash_ex2(s[n][q][2 + x] - ref);
           sum += s[n][q][x] + s[n][q][2 + x];
         }
-        l[q][x] = fmaf(l[q][x], alpha[x], sum);
+        l[q][x] = fmaf(l[q][x], alpha[q][x], sum);
       }
-      if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {       // a new maximum: seldom, after the first tiles
+    if (__any_sync(0xffffffffu, moved)) {          // a new maximum: seldom, after the first tiles
 #pragma unroll
-        for (int n = 0; n < D / 16; ++n) o[q][n][0] *= alpha[0], o[q][n][1] *= alpha[1], o[q][n][2] *= alpha[0], o[q][n][3] *= alpha[1];
-      }
+      for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int n = 0; n < D / 16; ++n) o[q][n][0] *= alpha[q][0], o[q][n][1] *= alpha[q][1], o[q][n][2] *= alpha[q][0], o[q][n][3] *= alpha[q][1];
     }
 
-    // Where some rows see a slot and others do not, a value that is not finite must not reach the others as 0 x NaN: such
+    // Whole boxes arrive: what lies in slots that no row sees must not reach the products as 0 x NaN.
+    unsigned char *const values = paged_smem + (vst - smem0) + wk * KEYS * PB;
+    if (TMA && valid != ~0ull) {
+      for (int w = lane; w < KEYS * D / 8; w += 32) {
+        const int at = w % (KEYS * PD / 8), key = at / (PD / 8);
+        if (!(valid >> (wk * KEYS + key) & 1)) *reinterpret_cast<uint4 *>(values + w / (KEYS * PD / 8) * C::PART_BYTES + at * 16) = make_uint4(0u, 0u, 0u, 0u);
+      }
+      __syncwarp();
+    }
+    // Where some rows see a slot and others do not, a value that is not finite must not reach the others either: such
     // slots (rare) leave the products and are added to the rows that see them.
     unsigned long long odd = 0;
     const int from = max(mine, len_lo), to = min(mine + KEYS, total);
     if (a.M > 1 && (max(from, min_end) < to || from < min(to, max_start))) {
-      const unsigned char *rows = paged_smem + (vst - smem0) + wk * KEYS * RB;
       uint32_t hit = 0;
 #pragma unroll
-      for (int w = 0; w < KEYS * RB / 512; ++w) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(rows + (w * 32 + lane) * 16);
+      for (int w = 0; w < KEYS * D / 256; ++w) {
+        const int at = w * 32 + lane;
+        const uint4 v = *reinterpret_cast<const uint4 *>(values + at / (KEYS * PD / 8) * C::PART_BYTES + at % (KEYS * PD / 8) * 16);
         // an exponent of ones, 0x7f80, plus 0x80 reaches the sign bit
         hit |= ((v.x & 0x7f807f80u) + 0x00800080u) | ((v.y & 0x7f807f80u) + 0x00800080u) | ((v.z & 0x7f807f80u) + 0x00800080u) | ((v.w & 0x7f807f80u) + 0x00800080u);
       }
@@ -277,12 +396,13 @@ __global__ void __launch_bounds__(PA_MMA_THREADS, PagedMma<D, NQ, WR>::CTAS) pag
 #pragma unroll 1
         for (int key = 0; key < KEYS; ++key) {
           hit = 0;
-          for (int w = lane; w < D / 2; w += 32) hit |= (reinterpret_cast<const uint32_t *>(rows + key * RB)[w] & 0x7f807f80u) + 0x00800080u;
+          for (int w = lane; w < D / 2; w += 32)
+            hit |= (*reinterpret_cast<const uint32_t *>(values + w / (PD / 2) * C::PART_BYTES + key * PB + w % (PD / 2) * 4) & 0x7f807f80u) + 0x00800080u;
           if (__any_sync(0xffffffffu, hit & 0x80008000u)) odd |= 1ull << key;
         }
       }
     }
-    const uint32_t va = vst + wk * KEYS * RB + value_at;
+    const uint32_t va = vst + wk * KEYS * PB + value_at;
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       uint32_t hi[NQ][2], lo[NQ][2];               // slots 2 t4, 2 t4 + 1 (+ 8) x query g, after the transposition
@@ -301,23 +421,31 @@ __global__ void __launch_bounds__(PA_MMA_THREADS, PagedMma<D, NQ, WR>::CTAS) pag
         mask0 = (bits & 1 ? 0u : 0xffffu) | (bits & 2 ? 0u : 0xffff0000u);
         mask1 = (bits & 256 ? 0u : 0xffffu) | (bits & 512 ? 0u : 0xffff0000u);
       }
+      constexpr int GROUP = D / 16 < 4 ? D / 16 : 4;              // products of the high parts, then of the low parts: none waits for the one before
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        uint32_t v[4];
-        flash_ldsm4_trans((va + n * 16 * RB) ^ (uint32_t)(ks * 32), v);
-        if (odd) v[0] &= mask0, v[1] &= mask0, v[2] &= mask1, v[3] &= mask1;
+      for (int k0 = 0; k0 < D / 16; k0 += GROUP) {
+        uint32_t v[GROUP][4];
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-          mma_bf16_16816(o[q][ks], v, hi[q][0], hi[q][1]);
-          mma_bf16_16816(o[q][ks], v, lo[q][0], lo[q][1]);
+        for (int j = 0; j < GROUP; ++j) {
+          const int ks = k0 + j;
+          flash_ldsm4_trans((va + n * 16 * PB + ks / (PD / 16) * C::PART_BYTES) ^ (uint32_t)(ks % (PD / 16) * 32), v[j]);
+          if (odd) v[j][0] &= mask0, v[j][1] &= mask0, v[j][2] &= mask1, v[j][3] &= mask1;
         }
+#pragma unroll
+        for (int j = 0; j < GROUP; ++j)
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) mma_bf16_16816(o[q][k0 + j], v[j], hi[q][0], hi[q][1]);
+#pragma unroll
+        for (int j = 0; j < GROUP; ++j)
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) mma_bf16_16816(o[q][k0 + j], v[j], lo[q][0], lo[q][1]);
       }
       if (odd) {
 #pragma unroll 1
         for (int key = 0; key < 16; ++key) {
           if (!(odd >> (n * 16 + key) & 1)) continue;
           const int slot = mine + n * 16 + key, row = wk * KEYS + n * 16 + key;
-          const unsigned char *value = paged_smem + (vst - smem0) + row * RB;
+          const unsigned char *value = paged_smem + (vst - smem0) + row * PB;
 #pragma unroll
           for (int q = 0; q < NQ; ++q)
 #pragma unroll
@@ -328,67 +456,101 @@ __global__ void __launch_bounds__(PA_MMA_THREADS, PagedMma<D, NQ, WR>::CTAS) pag
               for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
-                  o[q][ks][2 * e + x] = fmaf(p, to_f32(*reinterpret_cast<const bf16 *>(value + flash_swz<D>(row, 2 * ks + e) * 16 + g * 2)), o[q][ks][2 * e + x]);
+                  o[q][ks][2 * e + x] = fmaf(p, to_f32(*reinterpret_cast<const bf16 *>(value + ks / (PD / 16) * C::PART_BYTES + flash_swz<PD>(row, (2 * ks + e) % (PD / 8)) * 16 + g * 2)), o[q][ks][2 * e + x]);
             }
         }
       }
     }
 
     if (it.t + 1 == tiles || i + 1 == run.count) {
-      // the unit, or this CTA's part of it, ends: all warps' parts through this stage's memory, then the result by all threads
-      const int rows = min(ROWS, R - row0);
-      bar_sync(MERGE, PA_THREADS);
-      float *scratch = reinterpret_cast<float *>(paged_smem + stage * C::STAGE_BYTES);        // [warp][row][D + 4]
-      float2 *ml_scratch = reinterpret_cast<float2 *>(scratch + 4 * WROWS * C::MERGE_ROW);    // [warp][row]
+      // the unit, or this CTA's part of it, ends: the other warps' parts through this stage's memory, in the fragments' order
 #pragma unroll
       for (int q = 0; q < NQ; ++q)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const int r = q * 8 + t4 * 2 + x;
-          float sum = l[q][x];
-          sum += __shfl_xor_sync(0xffffffffu, sum, 4);
-          sum += __shfl_xor_sync(0xffffffffu, sum, 8);
-          sum += __shfl_xor_sync(0xffffffffu, sum, 16);
-          if (wr * WROWS + r < rows) {
-            if (g == 0) ml_scratch[warp * WROWS + r] = make_float2(m[q][x], sum);
+          l[q][x] += __shfl_xor_sync(0xffffffffu, l[q][x], 4);
+          l[q][x] += __shfl_xor_sync(0xffffffffu, l[q][x], 8);
+          l[q][x] += __shfl_xor_sync(0xffffffffu, l[q][x], 16);
+        }
+      if (WK > 1) {
+        bar_sync(MERGE, 32 * C::WARPS);
+        float4 *scratch = reinterpret_cast<float4 *>(paged_smem + stage * C::STAGE_BYTES) + lane;
+        constexpr int WORDS = 32 * C::MERGE_WORDS;
+        if (wk) {
+          scratch += (wr * (WK - 1) + wk - 1) * WORDS;
 #pragma unroll
-            for (int n = 0; n < D / 16; ++n) {
-              scratch[(warp * WROWS + r) * C::MERGE_ROW + n * 16 + g] = o[q][n][x];
-              scratch[(warp * WROWS + r) * C::MERGE_ROW + n * 16 + g + 8] = o[q][n][2 + x];
+          for (int q = 0; q < NQ; ++q) {
+            scratch[32 * q] = make_float4(m[q][0], m[q][1], l[q][0], l[q][1]);
+#pragma unroll
+            for (int n = 0; n < D / 16; ++n) scratch[32 * (NQ + q * (D / 16) + n)] = make_float4(o[q][n][0], o[q][n][1], o[q][n][2], o[q][n][3]);
+          }
+        }
+        bar_sync(MERGE, 32 * C::WARPS);
+        if (!wk) {
+#pragma unroll 1
+          for (int w = 0; w < WK - 1; ++w) {
+            const float4 *src = scratch + (wr * (WK - 1) + w) * WORDS;
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) {
+              const float4 ml = src[32 * q];
+              const float top0 = fmaxf(m[q][0], ml.x), top1 = fmaxf(m[q][1], ml.y);
+              const float ref0 = top0 == -INFINITY ? 0.f : top0, ref1 = top1 == -INFINITY ? 0.f : top1;
+              const float a0 = exp2f(m[q][0] - ref0), a1 = exp2f(m[q][1] - ref1), b0 = exp2f(ml.x - ref0), b1 = exp2f(ml.y - ref1);
+              m[q][0] = top0, m[q][1] = top1;
+              l[q][0] = l[q][0] * a0 + ml.z * b0, l[q][1] = l[q][1] * a1 + ml.w * b1;
+#pragma unroll
+              for (int n = 0; n < D / 16; ++n) {
+                const float4 v = src[32 * (NQ + q * (D / 16) + n)];
+                o[q][n][0] = o[q][n][0] * a0 + v.x * b0, o[q][n][1] = o[q][n][1] * a1 + v.y * b1;
+                o[q][n][2] = o[q][n][2] * a0 + v.z * b0, o[q][n][3] = o[q][n][3] * a1 + v.w * b1;
+              }
             }
           }
         }
-      bar_sync(MERGE, PA_THREADS);
-      const bool whole = seg_first == 0 && it.t + 1 == tiles;
-      const int part = 2 * blockIdx.x + (seg_first == 0);
-      for (int e = tid; e < rows * (D / 4); e += PA_THREADS) {
-        const int r = e / (D / 4), d = (e - r * (D / 4)) * 4, w0 = r / WROWS * WK, rl = r % WROWS;
-        float top = ml_scratch[w0 * WROWS + rl].x;
+      }
+      if (!wk) {
+        const int first_row = row0 + wr * WROWS;
+        if (seg_first == 0 && it.t + 1 == tiles) {
 #pragma unroll
-        for (int w = 1; w < WK; ++w) top = fmaxf(top, ml_scratch[(w0 + w) * WROWS + rl].x);
-        const float ref = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int q = 0; q < NQ; ++q) {
+            const float inv0 = l[q][0] == 0.f ? 0.f : 1.f / l[q][0], inv1 = l[q][1] == 0.f ? 0.f : 1.f / l[q][1];
+            const int row = first_row + q * 8 + g;         // after the transposition: query g, elements 2 t4, 2 t4 + 1 (+ 8)
+            const bool live = row < R && token_of(a, row) < n_new;
+            bf16 *out = live ? paged_out_row<bf16>(a, it.b, h, row, D) + t4 * 2 : nullptr;
 #pragma unroll
-        for (int w = 0; w < WK; ++w) {
-          const float2 ml = ml_scratch[(w0 + w) * WROWS + rl];
-          const float f = exp2f(ml.x - ref);
-          const float4 x = *reinterpret_cast<const float4 *>(scratch + ((w0 + w) * WROWS + rl) * C::MERGE_ROW + d);
-          sum = fmaf(ml.y, f, sum);
-          v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
-        }
-        if (!whole) {
-          *reinterpret_cast<float4 *>(a.part_o + ((long long)part * ROWS + r) * D + d) = v;
-          if (d == 0) a.part_ml[part * ROWS + r] = make_float2(top, sum);
-        } else if ((row0 + r) / a.group < n_new) {
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;
-          uint2 y = sum == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
-          *reinterpret_cast<uint2 *>(paged_out_row<bf16>(a, it.b, h, row0 + r, D) + d) = y;
-          if (d == 0) paged_write_lse(a, it.b, h, row0 + r, top, sum);
+            for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                // (an empty row's sums are 0, and 0 x inf cannot arise)
+                const uint32_t y = movmatrix_trans(pack_bf16x2(o[q][n][2 * e] * inv0, o[q][n][2 * e + 1] * inv1));
+                if (live) *reinterpret_cast<uint32_t *>(out + n * 16 + e * 8) = y;
+              }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const int r = first_row + q * 8 + t4 * 2 + x;
+              if (g == 0 && r < R && token_of(a, r) < n_new) paged_write_lse(a, it.b, h, r, m[q][x], l[q][x]);
+            }
+          }
+        } else {
+          const int part = 2 * blockIdx.x + (seg_first == 0);
+#pragma unroll
+          for (int q = 0; q < NQ; ++q)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const int r = wr * WROWS + q * 8 + t4 * 2 + x;
+              if (row0 + r >= R) continue;
+              float *dst = a.part_o + ((long long)part * ROWS + r) * D + g;
+#pragma unroll
+              for (int n = 0; n < D / 16; ++n) dst[n * 16] = o[q][n][x], dst[n * 16 + 8] = o[q][n][2 + x];
+              if (g == 0) a.part_ml[part * ROWS + r] = make_float2(m[q][x], l[q][x]);
+            }
         }
       }
     }
-    if (i + S < run.count) bar_arrive(EMPTY + stage, PA_MMA_THREADS);
+    if (i + S < run.count) {
+      if (TMA) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");        // zeros and sums that were written here, before the next tile
+      bar_arrive(EMPTY + stage, C::THREADS);
+    }
     if (++stage == S) stage = 0;
   }
 }

@@ -4,7 +4,7 @@
 
 namespace tsfm {
 
-constexpr int BAD_ID = 1, BAD_LEN = 2;            // TSFM_PAGES_BAD_*
+constexpr int BAD_ID = 1, BAD_LEN = 2, PAGES_TIMEOUT = 4;      // TSFM_PAGES_*
 
 struct PagesDev {
   char *k, *v;

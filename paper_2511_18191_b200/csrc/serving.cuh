@@ -67,21 +67,30 @@ struct PagedPlan {
   size_t part_ml, part_o, lse2, scores, bytes;
   long long score_stride;
 };
+// The kernel of `rows` rows: eights of a warp, warps of a tile's rows.
+template <int D, typename F> auto paged_variant(int rows, F f) {
+  if (rows == 8) return f(PagedMma<D, 1, 1>());
+  if (rows == 16) return f(PagedMma<D, 2, 1>());
+  return f(PagedMma<D, 2, 2>());
+}
+template <int D> int paged_ctas(int rows) {
+  return paged_variant<D>(rows, [](auto c) { return decltype(c)::CTAS; });
+}
 int paged_plan(PagedPlan *pl, const tsfm_kv_pages *p, int B, int M, int n_heads, int max_len, bool weights) {
   if (int rc = pages_shape(p)) return rc;
   if (B < 1 || M < 1 || n_heads < 1 || max_len < 1) return TSFM_ERR_ARG;
   if (n_heads % p->n_kv_heads) return TSFM_ERR_SHAPE;
   const long long R = (long long)M * (n_heads / p->n_kv_heads), pairs = (long long)B * p->n_kv_heads;
-  if (max_len > kMaxSlots || R > 1 << 20 || pairs > kMaxGridX || (long long)B * M > kMaxGridX) return TSFM_ERR_SHAPE;
+  if (max_len > kMaxSlots || R > 65535 || pairs > kMaxGridX || (long long)B * M > kMaxGridX) return TSFM_ERR_SHAPE;
   // rows of a unit: fp32 what a thread's registers hold, bf16 16 to a warp
   int ctas = PA_F32_CTAS;
   if (p->dtype == TSFM_BF16) {
-    pl->rows = R <= 8 ? 8 : R <= 16 ? 16 : R <= 32 ? 32 : 64;
-    auto of = [&](auto d) {
-      constexpr int D = decltype(d)::value;
-      return R <= 8 ? PagedMma<D, 1, 1>::CTAS : R <= 16 ? PagedMma<D, 2, 1>::CTAS : R <= 32 ? PagedMma<D, 2, 2>::CTAS : PagedMma<D, 2, 4>::CTAS;
-    };
-    ctas = p->d_head == 32 ? of(std::integral_constant<int, 32>()) : p->d_head == 64 ? of(std::integral_constant<int, 64>()) : of(std::integral_constant<int, 128>());
+    pl->rows = R <= 8 ? 8 : R <= 16 ? 16 : 32;
+    switch (p->d_head) {
+      case 32: ctas = paged_ctas<32>(pl->rows); break;
+      case 64: ctas = paged_ctas<64>(pl->rows); break;
+      default: ctas = paged_ctas<128>(pl->rows);
+    }
   } else {
     pl->rows = R == 1 ? 1 : R == 2 ? 2 : 4;
   }
@@ -100,20 +109,42 @@ int paged_plan(PagedPlan *pl, const tsfm_kv_pages *p, int B, int M, int n_heads,
   return TSFM_OK;
 }
 
-template <int D, int NQ, int WR>
-cudaError_t launch_paged_mma(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl) {
-  using C = PagedMma<D, NQ, WR>;
+// Maps of the pool for TMA: {element, slot, head, page}, boxes of 64 (32) elements and up to 64 slots of a page.  False where
+// the driver has no encoder or refuses the pool's strides.
+bool paged_maps(CUtensorMap *k, CUtensorMap *v, const PagesDev &pg, int D) {
+  static const PFN_encodeTiled encode = [] {
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult res{};
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &res) != cudaSuccess || res != cudaDriverEntryPointSuccess) fn = nullptr;
+    return (PFN_encodeTiled)fn;
+  }();
+  if (!encode) return false;
+  const cuuint32_t page = 1u << pg.page_log;
+  const cuuint64_t dims[4] = {(cuuint64_t)D, page, (cuuint64_t)pg.n_kv_heads, (cuuint64_t)pg.n_pages};
+  const cuuint64_t strides[3] = {(cuuint64_t)pg.slot_stride, (cuuint64_t)pg.head_stride, (cuuint64_t)pg.page_stride};
+  const cuuint32_t box[4] = {(cuuint32_t)std::min(D, 64), std::min(page, 64u), 1, 1}, one[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 2; ++i)
+    if (encode(i ? v : k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, i ? pg.v : pg.k, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               D == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return false;
+  return true;
+}
+
+template <typename C, bool TMA>
+cudaError_t launch_paged_mma(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl, const CUtensorMap &k, const CUtensorMap &v) {
   // (the attribute belongs to the device's context: set with every call, 0.2 us)
-  if (cudaError_t e = cudaFuncSetAttribute(paged_attn_mma_kernel<D, NQ, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES)) return e;
-  paged_attn_mma_kernel<D, NQ, WR><<<pl.grid, PA_MMA_THREADS, C::SMEM_BYTES, s>>>(a);
+  if (cudaError_t e = cudaFuncSetAttribute(paged_attn_mma_kernel<C, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES)) return e;
+  paged_attn_mma_kernel<C, TMA><<<pl.grid, C::THREADS, C::SMEM_BYTES, s>>>(a, k, v);
   return cudaGetLastError();
 }
 template <int D>
 cudaError_t launch_paged_rows(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl, bf16) {
-  return pl.rows == 8    ? launch_paged_mma<D, 1, 1>(s, a, pl)
-         : pl.rows == 16 ? launch_paged_mma<D, 2, 1>(s, a, pl)
-         : pl.rows == 32 ? launch_paged_mma<D, 2, 2>(s, a, pl)
-                         : launch_paged_mma<D, 2, 4>(s, a, pl);
+  CUtensorMap k{}, v{};
+  const bool tma = a.pg.page_log >= 3 && paged_maps(&k, &v, a.pg, D);
+  return paged_variant<D>(pl.rows, [&](auto c) {
+    using C = decltype(c);
+    return tma ? launch_paged_mma<C, true>(s, a, pl, k, v) : launch_paged_mma<C, false>(s, a, pl, k, v);
+  });
 }
 template <int D>
 cudaError_t launch_paged_rows(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl, float) {
@@ -241,6 +272,7 @@ int tsfm_paged_attention(void *stream, const tsfm_kv_pages *pages, const void *q
   a.M = M;
   a.n_heads = n_heads;
   a.group = n_heads / pages->n_kv_heads;
+  a.group_magic = (uint32_t)(((1ull << 32) + a.group - 1) / a.group);
   a.scale2 = scale * 1.4426950408889634f;
   a.causal = causal != 0;
   a.window = window;
