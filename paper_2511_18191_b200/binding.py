@@ -183,9 +183,10 @@ def _ptr(t) -> Optional[int]:
     """Address of a torch tensor / numpy array (None -> NULL)."""
     if t is None:
         return None
-    if isinstance(t, np.ndarray):
+    try:
+        return t.data_ptr()
+    except AttributeError:
         return t.ctypes.data
-    return t.data_ptr()
 
 
 def _arch(a) -> tsfm_arch:

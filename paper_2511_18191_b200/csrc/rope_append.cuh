@@ -29,81 +29,94 @@ __device__ __forceinline__ float2 rope_cos_sin(uint64_t turn, long long t, float
 }
 
 // A unit is what a thread turns at once in a head: with `half` a vector of the first half and its partner (or a vector
-// behind the turned part), interleaved a vector.  A thread keeps its unit and goes over tokens and heads, so that the
-// angles of a unit are read once a token.
+// behind the turned part), interleaved a vector.  A thread keeps its unit and goes over the token's heads, so that the
+// angles of a unit are read once; the first two heads are on their way while the angles are computed.
 template <typename T, bool HALF>
 __global__ void __launch_bounds__(256) rope_append_kernel(const __grid_constant__ RopeAppendArgs a, int D) {
-  constexpr int V = Pack16<T>::N;
+  constexpr int V = Pack16<T>::N, N = 2;           // heads in flight
   extern __shared__ float2 cs[];                                 // [token lane][pair]
   const int vecs = D / V, half_vecs = a.pairs / V;
   const int units = HALF ? vecs - half_vecs : vecs;
   const int u = threadIdx.x % units, rest = threadIdx.x / units;
   const int hl = rest % a.head_lanes, tl = rest / a.head_lanes;
   const int Hkv = a.pg.n_kv_heads, heads = a.n_heads + 2 * Hkv;
-  const int t0 = blockIdx.x * a.token_lanes;
-  for (int i = threadIdx.x; i < a.token_lanes * a.pairs; i += blockDim.x) {
-    const int lane = i / a.pairs, p = i - lane * a.pairs, tok = t0 + lane;
-    if (tok < a.tokens) {
-      const int b = tok / a.M, m = tok - b * a.M;
-      cs[i] = rope_cos_sin(a.turn[p], (long long)(a.pos ? a.pos[b] : a.len[b]) + m, a.mscale);
-    }
-  }
-  __syncthreads();
-  const int tok = t0 + tl;
-  if (tl >= a.token_lanes || tok >= a.tokens) return;
-  const int b = tok / a.M, m = tok - b * a.M;
-  if (a.n_new && m >= a.n_new[b]) return;
-  // the token's slot
-  const long long slot = (long long)a.len[b] + m;
-  int page = -1;
-  if (slot < 0 || slot >= a.pg.capacity) {
-    if (u == 0 && hl == 0) pages_report(a.pg, BAD_LEN);
-  } else {
-    page = page_of(a.pg, a.pg.table + (long long)b * a.pg.table_stride, (int)slot);
-    if (page < 0 && u == 0 && hl == 0) pages_report(a.pg, BAD_ID);
-  }
+  const int t0 = blockIdx.x * a.token_lanes, tok = t0 + tl;
   const int first = HALF && u >= half_vecs ? u + half_vecs : u;  // this unit's vectors of a head
   const bool pair = HALF && u < half_vecs;
   const int second = first + half_vecs;
+  const bool mine = tl < a.token_lanes && tok < a.tokens;
+  const int b = mine ? tok / a.M : 0, m = tok - b * a.M;
+  const T *src = reinterpret_cast<const T *>(a.qkv) + (long long)(mine ? tok : 0) * a.qkv_stride;
+  Pack16<T> x[N], y[N];
+  auto fetch = [&](int h) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const T *s = src + (h + j * a.head_lanes) * D;
+      if (mine && h + j * a.head_lanes < heads) {
+        x[j].raw = *reinterpret_cast<const uint4 *>(s + first * V);
+        if (pair) y[j].raw = *reinterpret_cast<const uint4 *>(s + second * V);
+      }
+    }
+  };
+  int h = (a.q_out ? 0 : a.n_heads) + hl;
+  fetch(h);
+  for (int i = threadIdx.x; i < a.token_lanes * a.pairs; i += blockDim.x) {
+    const int at = i / a.pairs, p = i - at * a.pairs, t = t0 + at;
+    if (t < a.tokens) {
+      const int tb = t / a.M;
+      cs[i] = rope_cos_sin(a.turn[p], (long long)(a.pos ? a.pos[tb] : a.len[tb]) + t - tb * a.M, a.mscale);
+    }
+  }
+  const bool live = mine && (!a.n_new || m < a.n_new[b]);
+  // the token's slot
+  const long long slot = mine ? (long long)a.len[b] + m : 0;
+  int page = -1;
+  if (live) {
+    const bool in = slot >= 0 && slot < a.pg.capacity;
+    if (in) page = page_of(a.pg, a.pg.table + (long long)b * a.pg.table_stride, (int)slot);
+    if (page < 0 && u == 0 && hl == 0) pages_report(a.pg, in ? BAD_ID : BAD_LEN);
+  }
+  __syncthreads();
+  if (!live) return;
   const float2 *ang = cs + tl * a.pairs;
-  const T *src = reinterpret_cast<const T *>(a.qkv) + (long long)tok * a.qkv_stride;
   T *qdst = a.q_out ? reinterpret_cast<T *>(a.q_out) + (long long)tok * a.q_stride : nullptr;
-  for (int h = (a.q_out ? 0 : a.n_heads) + hl; h < heads; h += a.head_lanes) {
-    const T *s = src + h * D;
-    Pack16<T> x, y;
-    x.raw = *reinterpret_cast<const uint4 *>(s + first * V);
-    if (pair) y.raw = *reinterpret_cast<const uint4 *>(s + second * V);
-    if (h < a.n_heads + Hkv) {
-      if (pair) {
+  for (; h < heads; fetch(h += N * a.head_lanes)) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float2 c = ang[u * V + e];
-          const float p = x.get(e), q = y.get(e);
-          x.set(e, p * c.x - q * c.y);
-          y.set(e, q * c.x + p * c.y);
-        }
-      } else if (!HALF) {
+    for (int j = 0; j < N; ++j) {
+      const int hj = h + j * a.head_lanes;
+      if (hj >= heads) break;
+      if (hj < a.n_heads + Hkv) {
+        if (pair) {
 #pragma unroll
-        for (int e = 0; e < V; e += 2) {
-          if (u * V + e < 2 * a.pairs) {
-            const float2 c = ang[(u * V + e) >> 1];
-            const float p = x.get(e), q = x.get(e + 1);
-            x.set(e, p * c.x - q * c.y);
-            x.set(e + 1, q * c.x + p * c.y);
+          for (int e = 0; e < V; ++e) {
+            const float2 c = ang[u * V + e];
+            const float p = x[j].get(e), q = y[j].get(e);
+            x[j].set(e, p * c.x - q * c.y);
+            y[j].set(e, q * c.x + p * c.y);
+          }
+        } else if (!HALF) {
+#pragma unroll
+          for (int e = 0; e < V; e += 2) {
+            if (u * V + e < 2 * a.pairs) {
+              const float2 c = ang[(u * V + e) >> 1];
+              const float p = x[j].get(e), q = x[j].get(e + 1);
+              x[j].set(e, p * c.x - q * c.y);
+              x[j].set(e + 1, q * c.x + p * c.y);
+            }
           }
         }
       }
+      T *d;
+      if (hj < a.n_heads) {
+        d = qdst + hj * D;
+      } else {
+        if (page < 0) continue;
+        const bool key = hj < a.n_heads + Hkv;
+        d = reinterpret_cast<T *>((key ? a.pg.k : a.pg.v) + slot_offset(a.pg, page, hj - a.n_heads - (key ? 0 : Hkv), (int)slot));
+      }
+      *reinterpret_cast<uint4 *>(d + first * V) = x[j].raw;
+      if (pair) *reinterpret_cast<uint4 *>(d + second * V) = y[j].raw;
     }
-    T *d;
-    if (h < a.n_heads) {
-      d = qdst + h * D;
-    } else {
-      if (page < 0) continue;
-      const bool key = h < a.n_heads + Hkv;
-      d = reinterpret_cast<T *>((key ? a.pg.k : a.pg.v) + slot_offset(a.pg, page, h - a.n_heads - (key ? 0 : Hkv), (int)slot));
-    }
-    *reinterpret_cast<uint4 *>(d + first * V) = x.raw;
-    if (pair) *reinterpret_cast<uint4 *>(d + second * V) = y.raw;
   }
 }
 
@@ -158,7 +171,8 @@ static void launch_rope_append(cudaStream_t s, RopeAppendArgs &a, int D) {
     return;
   }
   const int units = a.half ? (D - a.pairs) / V : D / V, heads = a.n_heads + 2 * a.pg.n_kv_heads;
-  a.head_lanes = heads < 256 / units ? heads : 256 / units;
+  const int rounds = (heads + 256 / units - 1) / (256 / units);      // of a thread over the heads; the same number for each
+  a.head_lanes = (heads + rounds - 1) / rounds;
   a.token_lanes = 256 / (units * a.head_lanes);
   if (a.token_lanes > a.tokens) a.token_lanes = a.tokens;
   const int threads = (units * a.head_lanes * a.token_lanes + 31) / 32 * 32;

@@ -356,12 +356,15 @@ int tsfm_verify_tokens(void *stream, const int32_t *tokens, const float *p, int6
   a.out = out;
   a.n_accept = n_accept;
   a.len_out = len_out;
+  // CTAs of a series: enough for the SMs, but not for less than 2048 entries each.  Sixteen warps each where few fill the GPU, else
+  // eight, of which an SM holds eight: less is lost in the last wave.
   int cluster = 1;
-  while (cluster < VERIFY_MAX_CLUSTER && (long long)B * cluster < 2 * kSms && V / cluster > 4096) cluster *= 2;
+  while (cluster < VERIFY_MAX_CLUSTER && (long long)B * cluster < 6 * kSms && V / cluster > 4096) cluster *= 2;
+  const int warps = (long long)B * cluster <= 2 * kSms ? VERIFY_MAX_WARPS : VERIFY_MAX_WARPS / 2;
   if ((long long)B * cluster > kMaxGridX) return TSFM_ERR_SHAPE;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(B * cluster));
-  cfg.blockDim = dim3(VERIFY_THREADS);
+  cfg.blockDim = dim3(32 * warps);
   cfg.stream = (cudaStream_t)stream;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
