@@ -356,11 +356,11 @@ int tsfm_verify_tokens(void *stream, const int32_t *tokens, const float *p, int6
   a.out = out;
   a.n_accept = n_accept;
   a.len_out = len_out;
-  // CTAs of a series: enough for the SMs, but not for less than 2048 entries each.  Sixteen warps each where few fill the GPU, else
-  // eight, of which an SM holds eight: less is lost in the last wave.
-  int cluster = 1;
-  while (cluster < VERIFY_MAX_CLUSTER && (long long)B * cluster < 6 * kSms && V / cluster > 4096) cluster *= 2;
-  const int warps = (long long)B * cluster <= 2 * kSms ? VERIFY_MAX_WARPS : VERIFY_MAX_WARPS / 2;
+  // All CTAs resident at once where that is possible, 32 warps on an SM in CTAs of four (256 rows of 100003: 4 CTAs of 4 warps each,
+  // 7 on an SM; 2 of 8, 3 or 4 on an SM, took a fifth longer); fewer rows get more warps, of 512 entries at least.
+  int cluster = 1, warps = 4;
+  while (cluster < VERIFY_MAX_CLUSTER && 2ll * B * cluster <= 8 * kSms && V > cluster * 4096) cluster *= 2;
+  while (warps < VERIFY_MAX_WARPS && 2ll * B * cluster * warps <= 32 * kSms && V > cluster * warps * 512) warps *= 2;
   if ((long long)B * cluster > kMaxGridX) return TSFM_ERR_SHAPE;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(B * cluster));

@@ -18,8 +18,11 @@ struct VerifyArgs {
   int *out, *n_accept, *len_out;
 };
 
-// A probability as a weight of the draw: what is negative or not finite counts as 0.
-__device__ __forceinline__ float draw_weight(float p) { return p > 0.f && p < INFINITY ? p : 0.f; }
+constexpr int VERIFY_MAX_WARPS = 16, VERIFY_MAX_CLUSTER = 8, VERIFY_BATCH = 256;
+
+// A probability as a weight of the draw: what is negative or not finite counts as 0.  (The bits of a positive finite float are
+// 1 .. 0x7f7fffff.)
+__device__ __forceinline__ float draw_weight(float p) { return __float_as_uint(p) - 1u < 0x7f7fffffu ? p : 0.f; }
 
 // What a token is drawn from: max(p - q, 0) for a row q, p without one token (q is 1 there), or p.
 struct DrawRow {
@@ -32,34 +35,68 @@ struct DrawRow {
     return (double)x - (double)fminf(x, draw_weight(q));
   }
   __device__ __forceinline__ double at(int t) const { return rest(p_at(t), q_at(t)); }
-  // The sum over [lo, hi) by a warp, in all lanes.  Sixteen loads of a lane in flight: with what the compiler had gathered by
-  // itself the batch of 256 rows of 100003 took 132 us.
-  __device__ __forceinline__ double sum(int lo, int hi, int lane) const { return q ? sum_of<true>(lo, hi, lane) : sum_of<false>(lo, hi, lane); }
-  template <bool Q> __device__ __forceinline__ double sum_of(int lo, int hi, int lane) const {
-    constexpr int N = 8;
-    double s[4] = {0, 0, 0, 0};
-    for (int t0 = lo + lane; t0 < hi; t0 += 32 * N) {
-      float x[N], y[N];
+  // Sums over [lo, hi) by a warp, one of every `length` entries (a multiple of 256) into seg[], and all of them, in all lanes.
+  // Sixteen loads of a lane in flight: with what the compiler had gathered by itself the batch of 256 rows of 100003 took 132 us.
+  __device__ __forceinline__ double sums(int lo, int hi, int length, int lane, double *seg) const {
+    return q ? sums_of<true>(lo, hi, length, lane, seg) : sums_of<false>(lo, hi, length, lane, seg);
+  }
+  template <bool Q> __device__ __forceinline__ double sums_of(int lo, int hi, int length, int lane, double *seg) const {
+    constexpr int N = VERIFY_BATCH / 32;
+    double total = 0;
+    const float *pt = p + lo + lane, *qt = Q ? q + lo + lane : nullptr;
+    for (int k = 0; lo < hi; ++k) {
+      double s[4] = {0, 0, 0, 0};
+      for (const int end = min(hi, lo + length); lo < end; lo += VERIFY_BATCH, pt += VERIFY_BATCH, qt += Q ? VERIFY_BATCH : 0) {
+        const int t = lo + lane;
+        float x[N], y[N];
+        if (lo + VERIFY_BATCH <= hi) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const int t = t0 + 32 * e;
-        x[e] = t < hi ? p_at(t) : 0.f;
-        y[e] = Q ? (t < hi ? __ldg(q + t) : 0.f) : t == without ? 1.f : 0.f;
+          for (int e = 0; e < N; ++e) x[e] = __ldg(pt + 32 * e);
+#pragma unroll
+          for (int e = 0; e < N; ++e) y[e] = Q ? __ldg(qt + 32 * e) : t + 32 * e == without ? 1.f : 0.f;
+        } else {
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            const bool in = t + 32 * e < hi;
+            x[e] = in ? __ldg(pt + 32 * e) : 0.f;
+            y[e] = Q ? (in ? __ldg(qt + 32 * e) : 0.f) : t + 32 * e == without ? 1.f : 0.f;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) s[e & 3] += rest(x[e], y[e]);
       }
-#pragma unroll
-      for (int e = 0; e < N; ++e) s[e & 3] += rest(x[e], y[e]);
+      const double sum = warp_sum_d((s[0] + s[1]) + (s[2] + s[3]));
+      if (lane == 0) seg[k] = sum;
+      total += sum;
     }
-    return warp_sum_d((s[0] + s[1]) + (s[2] + s[3]));
+    return total;
   }
 };
 
-// A cluster of CTAs a series; CTA c, and in it each warp, sums a contiguous part of the row.  Everything after the sums
-// happens in the CTA, then the warp, whose part the draw falls into.  Sums are fp64 so that their order decides nothing.
-constexpr int VERIFY_MAX_WARPS = 16, VERIFY_MAX_CLUSTER = 8, VERIFY_LAST = 512;
-__global__ void __launch_bounds__(32 * VERIFY_MAX_WARPS) verify_tokens_kernel(VerifyArgs a) {
+// The first of n parts that ends above the target, the last one with weight should rounding leave none; base: what lies before it.
+__device__ __forceinline__ int part_of(const double *part, int n, double target, double &base) {
+  int at = 0;
+  double before = base;
+  for (int i = 0; i < n; ++i) {
+    const double s = part[i];
+    if (!(s > 0)) continue;
+    at = i;
+    base = before;
+    before += s;
+    if (before > target) break;
+  }
+  return at;
+}
+
+// A cluster of CTAs a series; CTA c, and in it each warp, sums a contiguous part of the row, and keeps the sums of up to 32
+// segments of it.  The draw then falls into a CTA's, a warp's, a segment's part: 256 entries for rows of up to 32 x 256 a warp, which one
+// warp looks through; a longer segment is shared by the CTA's warps as the row was.  Sums are fp64 so that their order decides nothing.
+// Bound: memory, behind the chain proposals - their probabilities - row.  (In place of the segments' sums three more passes over ever
+// smaller parts cost 10 us.)
+__global__ void __launch_bounds__(32 * VERIFY_MAX_WARPS, 2) verify_tokens_kernel(VerifyArgs a) {
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
-  __shared__ double part[VERIFY_MAX_WARPS], all[2][VERIFY_MAX_CLUSTER];
+  __shared__ double part[VERIFY_MAX_WARPS], seg[VERIFY_MAX_WARPS][32], all[2][VERIFY_MAX_CLUSTER];
   __shared__ int first_bad;
   cluster.barrier_arrive();                        // (waited for before the first store to another CTA's shared memory)
   const int C = (int)cluster.num_blocks(), c = (int)cluster.block_rank(), b = blockIdx.x / C;
@@ -87,14 +124,19 @@ __global__ void __launch_bounds__(32 * VERIFY_MAX_WARPS) verify_tokens_kernel(Ve
   __syncthreads();
   const int n = first_bad;
   DrawRow row{p0 + n * a.p_stride, n < nd && q0 ? q0 + n * a.q_stride : nullptr, n < nd && !q0 ? a.tokens[(long long)b * K + n] : -1};
-  const int slice = (V + C - 1) / C, v0 = min(V, c * slice), v1 = min(V, v0 + slice);
-  const int step = (slice + warps - 1) / warps;
-  const int w0 = min(v1, v0 + warp * step), w1 = min(v1, w0 + step);
-  double total = 0, mine = 0;
+  const int slice = (V + C - 1) / C;
+  int lo = min(V, c * slice), hi = min(V, lo + slice), step = 0, length = 0;
+  auto level = [&]() {                             // [lo, hi) by the CTA's warps
+    const int each = ((hi - lo + warps - 1) / warps + VERIFY_BATCH - 1) / VERIFY_BATCH;
+    step = each * VERIFY_BATCH;
+    length = (each + 31) / 32 * VERIFY_BATCH;
+    const int w0 = (int)min((long long)hi, lo + (long long)warp * step), w1 = (int)min((long long)hi, (long long)w0 + step);
+    const double sum = row.sums(w0, w1, length, lane, seg[warp]);
+    if (lane == 0) part[warp] = sum;
+  };
 #pragma unroll 1
   for (int attempt = 0; attempt < 2; ++attempt) {
-    mine = row.sum(w0, w1, lane);
-    if (lane == 0) part[warp] = mine;
+    level();
     if (attempt == 0) cluster.barrier_wait();
     __syncthreads();
     if (warp == 0) {
@@ -103,83 +145,55 @@ __global__ void __launch_bounds__(32 * VERIFY_MAX_WARPS) verify_tokens_kernel(Ve
       if (lane < C) *cluster.map_shared_rank(&all[attempt][c], lane) = s;
     }
     cluster.sync();
-    total = 0;
+    double total = 0;
     for (int i = 0; i < C; ++i) total += all[attempt][i];
-    if (total > 0 || attempt == 1) {
-      double before = 0, target = 0;
-      const float u = uniform(K);
-      target = (double)fminf(fmaxf(u, 0.f), 0.999999940395355224609375f) * total;
-      // the CTA whose part holds the target (the last one with weight, should rounding leave none)
-      int owner = -1;
+    if (total > 0) {
+      const double target = (double)fminf(fmaxf(uniform(K), 0.f), 0.999999940395355224609375f) * total;
       double base = 0;
-      for (int i = 0; i < C; ++i) {
-        const double s = all[attempt][i];
-        if (!(s > 0)) continue;
-        owner = i;
-        base = before;
-        before += s;
-        if (before > target) break;
-      }
-      int drawn = -1;
-      if (owner == c) {
-        // the warp's part, then ever smaller parts shared by the CTA's warps, until one warp can take the rest
-        int lo = v0, width = step, end = v1;
+      if (part_of(all[attempt], C, target, base) != c) break;
 #pragma unroll 1
-        for (;;) {
-          int at = -1;
-          double sum = base, start = base;
-          for (int i = 0; i < warps; ++i) {
-            const double s = part[i];
-            if (!(s > 0)) continue;
-            at = i;
-            start = sum;
-            sum += s;
-            if (sum > target) break;
-          }
-          base = start;
-          lo += max(at, 0) * width;
-          end = min(end, lo + width);
-          if (width <= VERIFY_LAST) break;
-          width = (width + warps - 1) / warps;
-          const int x0 = min(end, lo + warp * width), x1 = min(end, x0 + width);
-          const double s = row.sum(x0, x1, lane);
-          __syncthreads();
-          if (lane == 0) part[warp] = s;
-          __syncthreads();
-        }
-        if (warp == 0) {
-          // a contiguous run of entries a lane
-          const int run = (end - lo + 31) / 32;
-          double s = 0;
-          for (int i = 0; i < run; ++i) {
-            const int t = lo + lane * run + i;
-            if (t < end) s += row.at(t);
-          }
-          double inc = s;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const double v = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += v;
-          }
-          const unsigned over = __ballot_sync(0xffffffffu, s > 0 && base + inc > target), some = __ballot_sync(0xffffffffu, s > 0);
-          const int who = over ? __ffs(over) - 1 : some ? 31 - __clz(some) : -1;
-          if (lane == who) {
-            double cum = base + (inc - s);
-            for (int i = 0; i < run; ++i) {
-              const int t = lo + lane * run + i;
-              if (t >= end) break;
-              const double x = row.at(t);
-              cum += x;
-              if (x > 0) drawn = t;
-              if (x > 0 && cum > target) break;
-            }
-            a.out[(long long)b * (K + 1) + n] = drawn;
-          }
-          if (who < 0 && lane == 0) a.out[(long long)b * (K + 1) + n] = -1;
-        }
-      } else if (owner < 0 && c == 0 && threadIdx.x == 0) {
-        a.out[(long long)b * (K + 1) + n] = -1;
+      for (;;) {
+        const int w = part_of(part, warps, target, base);
+        const int w0 = lo + w * step, w1 = min(hi, w0 + step);
+        const int k = part_of(seg[w], (w1 - w0 + length - 1) / length, target, base);
+        lo = w0 + k * length;
+        hi = min(w1, lo + length);
+        if (length == VERIFY_BATCH) break;
+        __syncthreads();
+        level();
+        __syncthreads();
       }
+      if (warp == 0) {
+        // eight entries a lane, in order
+        constexpr int N = VERIFY_BATCH / 32;
+        double x[N], s = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = lo + lane * N + e < hi ? row.at(lo + lane * N + e) : 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) s += x[e];
+        double inc = s;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const double v = __shfl_up_sync(0xffffffffu, inc, o);
+          if (lane >= o) inc += v;
+        }
+        const unsigned over = __ballot_sync(0xffffffffu, s > 0 && base + inc > target), some = __ballot_sync(0xffffffffu, s > 0);
+        if (lane == (over ? __ffs(over) - 1 : 31 - __clz(some))) {
+          double cum = base + (inc - s);
+          int drawn = -1;
+          bool done = false;
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            cum += x[e];
+            if (x[e] > 0 && !done) drawn = lo + lane * N + e, done = cum > target;
+          }
+          a.out[(long long)b * (K + 1) + n] = drawn;
+        }
+      }
+      break;
+    }
+    if (attempt == 1) {
+      if (c == 0 && threadIdx.x == 0) a.out[(long long)b * (K + 1) + n] = -1;
       break;
     }
     row.q = nullptr;                               // p nowhere above q: draw from p
