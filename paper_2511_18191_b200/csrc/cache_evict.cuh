@@ -29,34 +29,34 @@ __device__ __forceinline__ uint32_t weight_rank(float w) {
 
 // One CTA, or a cluster of them where it is long, a series and head.  Sinks and recent slots get a rank above all others; then the
 // budget-th largest rank by three rounds of counting, digits of 11, 11 and 10 bits from the top; then the kept slots' places.  A warp
-// owns a contiguous part of the slots, whose ranks stay in shared memory where they fit (16384 slots a CTA).  Bound: the chain of
+// owns a contiguous part of the slots, whose ranks stay in shared memory where they fit (16 slots a thread).  Bound: the chain of
 // rounds for one series, instructions for many (32 x 8 heads of up to 16384 slots).  Loops stay loops: with the ranks in
 // registers, hence every pass unrolled, fetching the code took longer than running it.  The counters have copies, by lane: the top
 // digits of a heavy-tailed distribution are few.
-constexpr int EVICT_THREADS = 1024, EVICT_WARPS = EVICT_THREADS / 32, EVICT_MAX_CLUSTER = 8;
-constexpr int EVICT_OWN = 16384;                   // slots that a CTA's shared memory holds
-constexpr int EVICT_BINS = 2048, EVICT_COPIES = 4;
+constexpr int EVICT_MAX_CLUSTER = 8, EVICT_BINS = 2048;
 
-struct EvictShared {
-  int bins[EVICT_COPIES][EVICT_BINS], warp_hi[EVICT_WARPS], warp_eq[EVICT_WARPS];
+template <int THREADS> struct EvictShared {
+  static constexpr int WARPS = THREADS / 32, OWN = 16 * THREADS, COPIES = THREADS / 256;       // OWN: slots that a CTA holds
+  int bins[COPIES][EVICT_BINS], warp_hi[WARPS], warp_eq[WARPS];
   int all_hi[EVICT_MAX_CLUSTER], all_eq[EVICT_MAX_CLUSTER];
   uint32_t found;
   int left;
-  uint2 mask[EVICT_OWN / 32];                      // of 32 slots: those above the threshold, those equal to it
-  uint32_t rank[EVICT_OWN];
+  uint2 mask[OWN / 32];                            // of 32 slots: those above the threshold, those equal to it
+  uint32_t rank[OWN];
 };
 
 // KEPT: all of the series' ranks are in shared memory.
-template <bool KEPT>
-__device__ __forceinline__ void evict_select(const EvictArgs &a, EvictShared &sh, const float *w, int n, int *kept) {
+template <bool KEPT, int THREADS>
+__device__ __forceinline__ void evict_select(const EvictArgs &a, EvictShared<THREADS> &sh, const float *w, int n, int *kept) {
+  constexpr int WARPS = EvictShared<THREADS>::WARPS, OWN = EvictShared<THREADS>::OWN, COPIES = EvictShared<THREADS>::COPIES;
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, C = (int)cluster.num_blocks(), c = (int)cluster.block_rank();
   const int lo = a.sinks, hi = n - a.recent;
-  const long long part = ((n + C * EVICT_WARPS - 1) / (C * EVICT_WARPS) + 31) / 32 * 32;
-  const int p0 = (int)min((long long)n, (c * EVICT_WARPS + warp) * part), p1 = (int)min((long long)n, p0 + part);
-  uint32_t *const own = sh.rank + warp * (EVICT_OWN / EVICT_WARPS) + lane;       // of slots p0 + lane, p0 + lane + 32, ..
-  uint2 *const masks = sh.mask + warp * (EVICT_OWN / 32 / EVICT_WARPS);
+  const long long part = ((n + C * WARPS - 1) / (C * WARPS) + 31) / 32 * 32;
+  const int p0 = (int)min((long long)n, (c * WARPS + warp) * part), p1 = (int)min((long long)n, p0 + part);
+  uint32_t *const own = sh.rank + warp * (OWN / WARPS) + lane;       // of slots p0 + lane, p0 + lane + 32, ..
+  uint2 *const masks = sh.mask + warp * (OWN / 32 / WARPS);
   auto rank_of = [&](int i) { return i < lo || i >= hi ? 0xffffffffu : weight_rank(w[i]); };
   if (KEPT) {
 #pragma unroll 8
@@ -79,22 +79,22 @@ __device__ __forceinline__ void evict_select(const EvictArgs &a, EvictShared &sh
     const int bits = round == 2 ? 10 : 11;
     const uint32_t above = round ? 0xffffffffu << shift : 0, digit = (1u << bits) - 1;       // bits that are known; the next ones
     shift -= bits;
-    for (int i = tid; i < EVICT_COPIES * EVICT_BINS / 4; i += EVICT_THREADS) reinterpret_cast<int4 *>(sh.bins)[i] = make_int4(0, 0, 0, 0);
+    for (int i = tid; i < COPIES * EVICT_BINS / 4; i += THREADS) reinterpret_cast<int4 *>(sh.bins)[i] = make_int4(0, 0, 0, 0);
     __syncthreads();
-    int *const bins = sh.bins[lane % EVICT_COPIES];
+    int *const bins = sh.bins[lane % COPIES];
     each([&](int, uint32_t r, bool in) {
       if (in && (r & above) == prefix) atomicAdd(bins + (r >> shift & digit), 1);
     });
     __syncthreads();
     // thread t owns the PER bins that are t-th from the top
-    constexpr int PER = EVICT_BINS / EVICT_THREADS;
+    constexpr int PER = EVICT_BINS / THREADS;
     const int top = EVICT_BINS - 1 - PER * tid;
     int mine[PER], sum = 0;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       mine[j] = 0;
 #pragma unroll
-      for (int k = 0; k < EVICT_COPIES; ++k) mine[j] += sh.bins[k][top - j];
+      for (int k = 0; k < COPIES; ++k) mine[j] += sh.bins[k][top - j];
     }
     if (C > 1) {
 #pragma unroll
@@ -146,7 +146,7 @@ __device__ __forceinline__ void evict_select(const EvictArgs &a, EvictShared &sh
   int hi_at = __reduce_add_sync(0xffffffffu, lane < warp ? sh.warp_hi[lane] : 0);
   int eq_at = __reduce_add_sync(0xffffffffu, lane < warp ? sh.warp_eq[lane] : 0);
   if (C > 1) {
-    if (warp == EVICT_WARPS - 1 && lane < C) {
+    if (warp == WARPS - 1 && lane < C) {
       *cluster.map_shared_rank(&sh.all_hi[c], lane) = hi_at + hi_n;
       *cluster.map_shared_rank(&sh.all_eq[c], lane) = eq_at + eq_n;
     }
@@ -176,11 +176,12 @@ __device__ __forceinline__ void evict_select(const EvictArgs &a, EvictShared &sh
 }
 
 // (a cluster only where the longest series needs more than one CTA's registers)
-__global__ void __launch_bounds__(EVICT_THREADS, 2) evict_select_kernel(EvictArgs a) {
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS, 2048 / THREADS) evict_select_kernel(EvictArgs a) {
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
   extern __shared__ __align__(16) unsigned char evict_smem[];
-  EvictShared &sh = *reinterpret_cast<EvictShared *>(evict_smem);
+  EvictShared<THREADS> &sh = *reinterpret_cast<EvictShared<THREADS> *>(evict_smem);
   const int C = (int)cluster.num_blocks(), c = (int)cluster.block_rank(), pair = blockIdx.x / C;
   const int Hkv = a.pg.n_kv_heads, b = pair / Hkv, tid = threadIdx.x;
   const int raw = a.len[b], n = cut(raw, a.pg.capacity);
@@ -191,12 +192,12 @@ __global__ void __launch_bounds__(EVICT_THREADS, 2) evict_select_kernel(EvictArg
   }
   const float *w = a.w + pair * a.w_stride;
   int *kept = a.kept + (long long)pair * a.budget;
-  for (int j = keep + c * EVICT_THREADS + tid; j < a.budget; j += C * EVICT_THREADS) kept[j] = -1;
+  for (int j = keep + c * THREADS + tid; j < a.budget; j += C * THREADS) kept[j] = -1;
   if (n <= a.budget) {
-    for (int j = c * EVICT_THREADS + tid; j < n; j += C * EVICT_THREADS) kept[j] = j;
+    for (int j = c * THREADS + tid; j < n; j += C * THREADS) kept[j] = j;
   } else {
     if (C > 1) cluster.sync();                     // (all of them run before one reads another's shared memory)
-    if (n <= C * EVICT_OWN) evict_select<true>(a, sh, w, n, kept);
+    if (n <= C * sh.OWN) evict_select<true>(a, sh, w, n, kept);
     else evict_select<false>(a, sh, w, n, kept);
     if (C > 1) cluster.sync();                     // (nor leaves before)
   }

@@ -341,11 +341,17 @@ int tsfm_cache_evict(void *stream, const tsfm_kv_pages *pages, const int32_t *ds
   a.len_out = len_out;
   a.vecs = pages->d_head * (int)elt_bytes(pages->dtype) / 16;
   cudaStream_t s = (cudaStream_t)stream;
-  // CTAs of a cluster: what the longest series' ranks need, as far as that goes
+  // threads, and above 16384 slots CTAs of a cluster: what the longest series' ranks need, as far as that goes
+  const int threads = a.pg.capacity <= 4096 ? 256 : a.pg.capacity <= 8192 ? 512 : 1024;
   int cluster = 1;
-  while (cluster < EVICT_MAX_CLUSTER && cluster * EVICT_OWN < a.pg.capacity && 2 * pairs * cluster <= kMaxGridX) cluster *= 2;
-  CU_TRY(cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(EvictShared)));
-  CU_TRY(launch_cluster(s, (unsigned)(pairs * cluster), EVICT_THREADS, sizeof(EvictShared), cluster, evict_select_kernel, a));
+  while (cluster < EVICT_MAX_CLUSTER && cluster * 16 * threads < a.pg.capacity && 2 * pairs * cluster <= kMaxGridX) cluster *= 2;
+  auto select = [&](auto kernel, size_t smem) {
+    if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) return e;
+    return launch_cluster(s, (unsigned)(pairs * cluster), threads, smem, cluster, kernel, a);
+  };
+  CU_TRY(threads == 256   ? select(evict_select_kernel<256>, sizeof(EvictShared<256>))
+         : threads == 512 ? select(evict_select_kernel<512>, sizeof(EvictShared<512>))
+                          : select(evict_select_kernel<1024>, sizeof(EvictShared<1024>)));
   LAUNCHED();
   // four rows a thread once that fills the SMs (32 x 8 heads of 2048: 114 us against 120 for the whole call), else two (1 x 4 of 1024:
   // 12.4 against 14.3)
