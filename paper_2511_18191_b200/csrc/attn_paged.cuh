@@ -11,9 +11,7 @@
 namespace tsfm {
 
 constexpr int PA_TILE = 64;                        // slots
-constexpr int PA_THREADS = 128;
 constexpr int PA_JOIN_WARPS = 8;
-constexpr int PA_F32_CTAS = 4;                     // on an SM
 
 // What a CTA that starts inside a unit leaves for the join: the unit, and the CTAs that share it.
 struct PagedMeta {
@@ -130,165 +128,6 @@ template <typename T>
 __device__ __forceinline__ T *paged_out_row(const PagedAttnArgs &a, int b, int h, int row, int D) {
   const int tok = token_of(a, row), head = h * a.group + row - tok * a.group;
   return reinterpret_cast<T *>(a.out) + ((long long)b * a.M + tok) * a.out_stride + (long long)head * D;
-}
-
-// The fp32 kernel.  Eight lanes share a slot, a warp works on four at a time, each group of eight lanes with its own running
-// maximum and sum; nothing is staged.
-template <int D, int ROWS>
-__global__ void __launch_bounds__(PA_THREADS) paged_attn_f32_kernel(const __grid_constant__ PagedAttnArgs a) {
-  constexpr int E = D / 8, V = 4, NV = E / V;                                       // elements a lane, of a load, loads
-  constexpr int WARPS = PA_THREADS / 32, KEYS = 2;                                  // slots of a group in flight
-  __shared__ float s_o[WARPS][ROWS][D];
-  __shared__ float2 s_ml[WARPS][ROWS];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l8 = lane & 7, grp = lane >> 3;
-  PagedRun run = paged_find_run<PA_THREADS>(a);
-  pdl_release();
-  if (threadIdx.x == 0) {
-    PagedMeta meta{-1, 0, 0, 0};
-    if (run.count > 0 && run.first) {
-      const int tiles = paged_span(a, run.b, false).tiles;
-      meta = PagedMeta{run.b, run.u, (int)(run.unit0 / run.per), (int)((run.unit0 + tiles - 1) / run.per)};
-    }
-    a.meta[blockIdx.x] = meta;
-  }
-  while (run.count > 0) {
-    const PagedSpan s = paged_span(a, run.b, false);
-    if (s.tiles == 0) {                                          // (a finished series: no units)
-      ++run.b, run.u = 0;
-      continue;
-    }
-    const int take = min(run.count, s.tiles - run.first);
-    const int h = run.u / a.chunks, row0 = (run.u - h * a.chunks) * ROWS, rows = min(ROWS, a.M * a.group - row0);
-    const int *table = a.pg.table + (long long)run.b * a.pg.table_stride;
-    float q[ROWS][E], o[ROWS][E], m[ROWS], l[ROWS];
-    int2 range[ROWS];
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      m[r] = -INFINITY;
-      l[r] = 0.f;
-      range[r] = r < rows ? paged_row_range(a, s, token_of(a, row0 + r)) : make_int2(0, 0);
-      const int tok = r < rows ? token_of(a, row0 + r) : 0, head = h * a.group + (r < rows ? row0 + r - tok * a.group : 0);
-      const float *src = reinterpret_cast<const float *>(a.q) + ((long long)run.b * a.M + tok) * a.q_stride + (long long)head * D;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        o[r][e] = 0.f;
-        q[r][e] = src[e / V * 8 * V + l8 * V + e % V];
-      }
-    }
-    for (int t = run.first; t < run.first + take; ++t) {
-      const int base = (s.tile0 + t) * PA_TILE + warp * (PA_TILE / WARPS);
-#pragma unroll 1
-      for (int i = 0; i < PA_TILE / WARPS; i += 4 * KEYS) {
-        float kx[KEYS][E], vx[KEYS][E];
-        bool live[KEYS];
-#pragma unroll
-        for (int j = 0; j < KEYS; ++j) {
-          const int slot = base + i + 4 * j + grp;
-          live[j] = slot < s.total && slot >= s.lo;
-          int page = -1;
-          if (live[j]) {
-            page = page_of(a.pg, table, slot);
-            if (page < 0) {
-              live[j] = false;
-              if (l8 == 0) pages_report(a.pg, BAD_ID);
-            }
-          }
-          const long long at = live[j] ? slot_offset(a.pg, page, h, slot) : 0;
-#pragma unroll
-          for (int n = 0; n < NV; ++n) {
-            float4 k4 = make_float4(0.f, 0.f, 0.f, 0.f), v4 = k4;
-            if (live[j]) {
-              k4 = *reinterpret_cast<const float4 *>(a.pg.k + at + (n * 8 + l8) * 16);
-              v4 = *reinterpret_cast<const float4 *>(a.pg.v + at + (n * 8 + l8) * 16);
-            }
-            kx[j][n * V] = k4.x, kx[j][n * V + 1] = k4.y, kx[j][n * V + 2] = k4.z, kx[j][n * V + 3] = k4.w;
-            vx[j][n * V] = v4.x, vx[j][n * V + 1] = v4.y, vx[j][n * V + 2] = v4.z, vx[j][n * V + 3] = v4.w;
-          }
-        }
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-          float sc[KEYS], top = m[r];
-#pragma unroll
-          for (int j = 0; j < KEYS; ++j) {
-            float d = 0.f;
-#pragma unroll
-            for (int e = 0; e < E; ++e) d = fmaf(q[r][e], kx[j][e], d);
-            d += __shfl_xor_sync(0xffffffffu, d, 1);
-            d += __shfl_xor_sync(0xffffffffu, d, 2);
-            d += __shfl_xor_sync(0xffffffffu, d, 4);
-            const int slot = base + i + 4 * j + grp;
-            sc[j] = live[j] && slot >= range[r].x && slot < range[r].y ? d * a.scale2 : -INFINITY;
-            top = fmaxf(top, sc[j]);
-            if (a.scores && l8 == 0 && r < rows && slot < s.total)
-              a.scores[(((long long)run.b * a.pg.n_kv_heads + h) * a.M * a.group + row0 + r) * a.score_stride + slot] = sc[j];
-          }
-          const float ref = top == -INFINITY ? 0.f : top, corr = exp2f(m[r] - ref);
-          float p[KEYS], sum = 0.f;
-#pragma unroll
-          for (int j = 0; j < KEYS; ++j) sum += p[j] = exp2f(sc[j] - ref);
-          m[r] = top;
-          l[r] = fmaf(l[r], corr, sum);
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            float v = o[r][e] * corr;
-            // (a slot that this row does not see may hold anything: 0 x NaN must not happen)
-#pragma unroll
-            for (int j = 0; j < KEYS; ++j) v = sc[j] == -INFINITY ? v : fmaf(p[j], vx[j][e], v);
-            o[r][e] = v;
-          }
-        }
-      }
-    }
-    // the four groups of a warp, then the warps
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-#pragma unroll
-      for (int x = 8; x < 32; x <<= 1) {
-        const float om = __shfl_xor_sync(0xffffffffu, m[r], x), ol = __shfl_xor_sync(0xffffffffu, l[r], x);
-        const float top = fmaxf(m[r], om), ref = top == -INFINITY ? 0.f : top;
-        const float f0 = exp2f(m[r] - ref), f1 = exp2f(om - ref);
-        m[r] = top;
-        l[r] = l[r] * f0 + ol * f1;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[r][e] = o[r][e] * f0 + __shfl_xor_sync(0xffffffffu, o[r][e], x) * f1;
-      }
-      if (grp == 0) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) s_o[warp][r][e / V * 8 * V + l8 * V + e % V] = o[r][e];
-        if (l8 == 0) s_ml[warp][r] = make_float2(m[r], l[r]);
-      }
-    }
-    __syncthreads();
-    const bool whole = run.first == 0 && take == s.tiles;
-    const int part = 2 * blockIdx.x + (run.first == 0);
-    for (int i = threadIdx.x; i < rows * D; i += PA_THREADS) {
-      const int r = i / D, d = i - r * D;
-      float top = s_ml[0][r].x;
-#pragma unroll
-      for (int w = 1; w < WARPS; ++w) top = fmaxf(top, s_ml[w][r].x);
-      const float ref = top == -INFINITY ? 0.f : top;
-      float sum = 0.f, v = 0.f;
-#pragma unroll
-      for (int w = 0; w < WARPS; ++w) {
-        const float f = exp2f(s_ml[w][r].x - ref);
-        sum = fmaf(s_ml[w][r].y, f, sum);
-        v = fmaf(s_o[w][r][d], f, v);
-      }
-      if (whole) {
-        if (token_of(a, row0 + r) < s.n_new) {
-          paged_out_row<float>(a, run.b, h, row0 + r, D)[d] = sum == 0.f ? 0.f : v / sum;
-          if (d == 0) paged_write_lse(a, run.b, h, row0 + r, top, sum);
-        }
-      } else {
-        a.part_o[((long long)part * ROWS + r) * D + d] = v;
-        if (d == 0) a.part_ml[part * ROWS + r] = make_float2(top, sum);
-      }
-    }
-    __syncthreads();
-    run.count -= take;
-    run.first = 0;
-    if (++run.u == a.units) run.u = 0, ++run.b;
-  }
 }
 
 // Joins the parts of the units that several CTAs shared: block x belongs to CTA x of the kernel before and works if that one is

@@ -4,15 +4,12 @@
 // WR x WK warps compute: a warp takes 8 NQ query rows against 64 / WK of a tile's slots, with a running maximum and sum of its own;
 // the WK warps of a row are merged when the unit ends.  Slots are the M side of the products and queries the N side (S^T = K Q^T,
 // O^T = V^T P^T, P^T by one 8 x 8 transposition per eight slots): rows come in eights, not sixteens, and eight cost half of the
-// instructions and registers.  One more warp fetches: a TMA copy of up to 64 slots of
-// a page, head and 64 elements (pages of less than eight slots, and pools that TMA has no map for: cp.async, a slot's row at a
-// time), and the queries of a unit's first tile, up to STAGES - 1 tiles ahead and across unit borders.  It alone waits for copies;
-// named barriers hand the stages over.  Precision: scores of bf16 operands in fp32; probabilities as two bf16 parts, so that only the
+// instructions and registers.  One more warp fetches (attn_paged_fetch.cuh).
+//  Precision: scores of bf16 operands in fp32; probabilities as two bf16 parts, so that only the
 // result is rounded.
 #pragma once
 #include "attn_narrow.cuh"
-#include "attn_paged.cuh"
-#include "gemm_tc.cuh"
+#include "attn_paged_fetch.cuh"
 
 namespace tsfm {
 
@@ -21,8 +18,6 @@ template <int D_, int NQ_, int WR_> struct PagedMma {
   static constexpr int WK = 2, KEYS = PA_TILE / WK, BLOCKS = KEYS / 16;
   static constexpr int WARPS = WR * WK, THREADS = 32 * WARPS + 32;
   static constexpr int WROWS = 8 * NQ, ROWS = WROWS * WR, RB = D * 2;
-  // keys and values of a stage: parts of 64 (32) elements, [part][slot], 16-byte chunks exchanged as TMA's 128-byte (64-byte)
-  // swizzle does, which is flash_swz of such rows
   static constexpr int PD = D < 64 ? D : 64, PARTS = D / PD, PB = PD * 2, PART_BYTES = PA_TILE * PB;
   static constexpr int KV_BYTES = PA_TILE * RB, Q_BYTES = ROWS * RB;
   // the merge, through one stage: a lane's float4s
@@ -36,43 +31,14 @@ template <int D_, int NQ_, int WR_> struct PagedMma {
   static constexpr int CTAS = D == 128 ? (BY_SMEM < 2 ? BY_SMEM : 2) : BY_SMEM < 4 ? BY_SMEM : 4;
 };
 
-// Barriers between the fetching warp and the others: `full` of a stage, `empty` of a stage; and one among the others.
-__device__ __forceinline__ void bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-__device__ __forceinline__ void bar_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-
-// A tile on its way: unit u of series b, its t-th tile, and the series' span.  first: the unit's queries come with it.
-struct PagedItem {
-  int b, u, t, first;
-  PagedSpan sp;
-};
-
-// TMA tile of a page's slots: {first element, slot, head, page}.
-__device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap *map, int x, int slot, int head, int page, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-      ::"r"(dst), "l"(map), "r"(x), "r"(slot), "r"(head), "r"(page), "r"(bar) : "memory");
-}
-// Bounded wait for a tile: false if it did not arrive within TC_WAIT_NS.
-__device__ __forceinline__ bool tile_arrived(uint32_t bar, uint32_t parity) {
-  unsigned long long t0 = 0;
-  for (uint32_t n = 0;; ++n) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if (n == 256) t0 = globaltimer_ns();
-    if (n > 256 && (n & 255) == 0 && globaltimer_ns() - t0 > TC_WAIT_NS) return false;
-  }
-}
-
 template <typename C, bool TMA>
 __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_mma_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV) {
   constexpr int D = C::D, NQ = C::NQ;
   constexpr int WK = C::WK, KEYS = C::KEYS, NB = C::BLOCKS, ROWS = C::ROWS, WROWS = C::WROWS, RB = C::RB, S = C::STAGES;
-  constexpr int FULL = 1, EMPTY = 1 + S, MERGE = 1 + 2 * S;
-  constexpr int PD = C::PD, PB = C::PB, PARTS = C::PARTS;
+  constexpr int FULL = bar_full(), EMPTY = bar_empty(S), MERGE = bar_merge(S);
+  constexpr int PD = C::PD, PB = C::PB;
   extern __shared__ __align__(1024) unsigned char paged_smem_raw[];
-  __shared__ alignas(8) unsigned long long s_full[S];                  // TMA's barriers, waited on by the fetching warp alone
-  __shared__ unsigned s_valid[S][2];               // slots of the tile that exist: in [lo, total), page in the pool
-  __shared__ PagedItem s_item[S], s_next[S];       // of the stages; of the tiles whose page ids are on their way
-  __shared__ int s_ids[S][TMA ? 8 : PA_TILE];      // those ids
+  __shared__ PagedStages<S, TMA> sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wr = warp / WK, wk = warp % WK;
   const int g = lane >> 2, t4 = lane & 3;
   const uint32_t smem0 = (smem_u32(paged_smem_raw) + 1023u) & ~1023u;
@@ -91,152 +57,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_mma_kernel(con
   if (run.count == 0) return;
 
   if (warp == C::WARPS) {
-    constexpr int CPR = D / 8, STEP = 32 / CPR;    // 16-byte chunks of a row; rows of a copy instruction
-    const int chunk = lane % CPR, sub = lane / CPR;
-    // Page ids travel like the tiles, AHEAD tiles before theirs and in the same groups: a plain load behind the queue of copies
-    // returned after 6000 to 17000 cycles and stood between each tile and the next.
-    constexpr int AHEAD = S - 1;
-    int b = run.b, u = run.u, t = run.first, ni = 0;
-    PagedSpan sp = paged_span(a, b, false);
-    int len_next = 0, new_next = 0;                // of series b + 1, looked at when it is reached
-    auto fetch_next = [&]() {
-      const int at = min(b + 1, a.B - 1);
-      len_next = __ldg(a.len + at);
-      new_next = a.n_new ? __ldg(a.n_new + at) : a.M;
-    };
-    fetch_next();
-    // TMA copies boxes of up to 64 slots of one page: a page id a box, else a slot
-    const int box_log = TMA ? min(a.pg.page_log, 6) : 0, boxes = PA_TILE >> box_log;
-    const uint32_t full0 = smem_u32(s_full);
-    bool dead = false;                             // a tile did not arrive: nothing more is fetched or waited for
-    if (TMA) {
-      if (lane < S) mbar_init(full0 + 8 * lane, 1);
-      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-    }
-    auto fetch_ids = [&]() {                       // of tile ni; then moves on
-      if (ni >= run.count) return;
-      const int ring = ni % S;
-      const int *row = a.pg.table + (long long)b * a.pg.table_stride;
-#pragma unroll
-      for (int x = 0; x < (TMA ? 1 : 2); ++x) {
-        const int j = 32 * x + lane, slot = (sp.tile0 + t) * PA_TILE + (j << box_log);
-        if (j < boxes && slot + (1 << box_log) > sp.lo && slot < sp.total)
-          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(&s_ids[ring][j])), "l"(row + (slot >> a.pg.page_log)) : "memory");
-      }
-      if (lane == 0) s_next[ring] = PagedItem{b, u, t, ni == 0 || t == 0, sp};
-      if (++ni == run.count) return;
-      if (++t == sp.tiles) {
-        t = 0;
-        if (++u == a.units) {
-          u = 0;
-          do {                                     // (there is one: the run goes on)
-            ++b;
-            sp = paged_span_of(a, len_next, new_next, false);
-            fetch_next();
-          } while (sp.tiles == 0);
-        }
-      }
-    };
-    for (int j = 0; j < AHEAD; ++j) fetch_ids();
-    flash_commit();
-    flash_wait<0>();
-    int stage = 0;
-    for (int i = 0; i < run.count; ++i) {
-      const uint32_t dst = smem0 + stage * C::STAGE_BYTES;
-      __syncwarp();
-      const PagedItem it = s_next[stage];
-      const int h = it.u / a.chunks;
-      const int base = (it.sp.tile0 + it.t) * PA_TILE;
-      long long off[2] = {-1, -1};                 // (plain copies) byte offsets of slots lane, lane + 32; -1: hidden
-      int page = -1;                               // (TMA) of box lane % 8
-      unsigned v[2];
-      if (TMA) {
-        const int j = lane & 7, slot = base + (j << box_log);
-        if (j < boxes && slot + (1 << box_log) > it.sp.lo && slot < it.sp.total) {
-          page = s_ids[stage][j];
-          if ((unsigned)page >= (unsigned)a.pg.n_pages) {
-            page = -1;
-            pages_report(a.pg, BAD_ID);
-          }
-        }
-        const unsigned ok = __ballot_sync(0xffffffffu, page >= 0) & 0xff;
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int at = 32 * x + lane;
-          v[x] = __ballot_sync(0xffffffffu, base + at >= it.sp.lo && base + at < it.sp.total && (ok >> (at >> box_log) & 1));
-        }
-      } else {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int slot = base + 32 * x + lane;
-          if (slot >= it.sp.lo && slot < it.sp.total) {
-            const int id = s_ids[stage][32 * x + lane];
-            if ((unsigned)id < (unsigned)a.pg.n_pages) off[x] = slot_offset(a.pg, id, h, slot);
-            else pages_report(a.pg, BAD_ID);
-          }
-          v[x] = __ballot_sync(0xffffffffu, off[x] >= 0);
-        }
-      }
-      __syncwarp();
-      fetch_ids();
-      if (i >= S) bar_sync(EMPTY + stage, C::THREADS);
-      if (lane == 0) {
-        s_valid[stage][0] = v[0], s_valid[stage][1] = v[1];
-        s_item[stage] = it;
-      }
-      if (TMA) {
-        const int part = (lane >> 3) % PARTS, kv = (lane >> 3) / PARTS;
-        const unsigned ok = __ballot_sync(0xffffffffu, page >= 0) & 0xff;
-        if (lane == 0 && !dead) mbar_expect_tx(full0 + 8 * stage, __popc(ok) * 2 * PARTS * (PB << box_log));
-        __syncwarp();
-        if (page >= 0 && kv < 2 && !dead) {
-          const int slot = base + ((lane & 7) << box_log);
-          tma_load_page(dst + kv * C::KV_BYTES + part * C::PART_BYTES + ((lane & 7) << box_log) * PB, kv ? &mapV : &mapK, part * PD,
-                        slot & ((1 << a.pg.page_log) - 1), h, page, full0 + 8 * stage);
-        }
-      } else {
-#pragma unroll
-        for (int r = 0; r < PA_TILE; r += STEP) {
-          const long long o = __shfl_sync(0xffffffffu, off[r / 32], (r & 31) + sub);
-          const uint32_t at = dst + (chunk / (PD / 8)) * C::PART_BYTES + (r + sub) * PB + flash_swz<PD>(r + sub, chunk % (PD / 8)) * 16;
-          const long long from = (o < 0 ? 0 : o) + chunk * 16;
-          const int bytes = o < 0 ? 0 : 16;        // hidden slots arrive as zeros
-          asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(at), "l"(a.pg.k + from), "r"(bytes) : "memory");
-          asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(at + C::KV_BYTES), "l"(a.pg.v + from), "r"(bytes) : "memory");
-        }
-      }
-      if (it.first) {
-        const int row0 = (it.u - h * a.chunks) * ROWS;
-#pragma unroll 4
-        for (int r = sub; r < ROWS; r += STEP) {
-          const bool in = row0 + r < R;
-          const int tok = in ? token_of(a, row0 + r) : 0, head = h * a.group + (in ? row0 + r - tok * a.group : 0);
-          const bf16 *src = reinterpret_cast<const bf16 *>(a.q) + ((long long)it.b * a.M + tok) * a.q_stride + (long long)head * D + chunk * 8;
-          const uint32_t at = dst + 2 * C::KV_BYTES + r * RB + flash_swz<D>(r, chunk) * 16;
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(src), "r"(in ? 16 : 0) : "memory");
-        }
-      }
-      flash_commit();
-      auto hand_over = [&](int tile) {
-        if (TMA && !dead && __any_sync(0xffffffffu, !tile_arrived(full0 + 8 * (tile % S), (tile / S) & 1))) {
-          dead = true;
-          pages_report(a.pg, PAGES_TIMEOUT);
-        }
-        __threadfence_block();
-        bar_arrive(FULL + tile % S, C::THREADS);
-      };
-      if (i >= S - 2) {
-        flash_wait<S - 2>();
-        hand_over(i - (S - 2));
-      }
-      if (i + 1 == run.count) {
-        flash_wait<0>();
-        for (int tile = max(0, run.count - (S - 2)); tile < run.count; ++tile) hand_over(tile);
-      }
-      if (++stage == S) stage = 0;
-    }
+    paged_fetch<C, TMA>(a, run, sh, smem0, mapK, mapV);
     return;
   }
 
@@ -250,7 +71,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_mma_kernel(con
 #pragma unroll 1
   for (int i = 0; i < run.count; ++i) {
     bar_sync(FULL + stage, C::THREADS);
-    const PagedItem it = s_item[stage];
+    const PagedItem it = sh.item[stage];
     const uint32_t kst = smem0 + stage * C::STAGE_BYTES, vst = kst + C::KV_BYTES;
     if (it.first) {
       const PagedSpan s = it.sp;
@@ -282,7 +103,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_mma_kernel(con
       }
     }
     const int base = (tile0 + it.t) * PA_TILE, mine = base + wk * KEYS;       // slots of the tile, of this warp
-    const unsigned long long valid = s_valid[stage][0] | (unsigned long long)s_valid[stage][1] << 32;
+    const unsigned long long valid = sh.valid[stage][0] | (unsigned long long)sh.valid[stage][1] << 32;
 
     // scores, slots x queries
     float s[NB][NQ][4];

@@ -2,6 +2,7 @@
 // shapes, workspace layout.
 #pragma once
 #include "attn_paged.cuh"
+#include "attn_paged_f32.cuh"
 #include "attn_paged_mma.cuh"
 #include "cache_evict.cuh"
 #include "pages.cuh"
@@ -83,14 +84,20 @@ struct PagedPlan {
   size_t part_ml, part_o, lse2, scores, bytes;
   long long score_stride;
 };
-// The kernel of `rows` rows: eights of a warp, warps of a tile's rows.
-template <int D, typename F> auto paged_variant(int rows, F f) {
-  if (rows == 8) return f(PagedMma<D, 1, 1>());
-  if (rows == 16) return f(PagedMma<D, 2, 1>());
-  return f(PagedMma<D, 2, 2>());
+// The kernel of `rows` rows: f gets its configuration.
+template <int D, typename F> auto paged_variant(bf16, int rows, F f) {
+  return rows == 8 ? f(PagedMma<D, 1, 1>()) : rows == 16 ? f(PagedMma<D, 2, 1>()) : f(PagedMma<D, 2, 2>());
 }
-template <int D> int paged_ctas(int rows) {
-  return paged_variant<D>(rows, [](auto c) { return decltype(c)::CTAS; });
+template <int D, typename F> auto paged_variant(float, int rows, F f) {
+  return rows == 1   ? f(PagedF32<D, 1, 1>())
+         : rows == 2 ? f(PagedF32<D, 2, 1>())
+         : rows == 4 ? f(PagedF32<D, 4, 1>())
+         : rows == 8 ? f(PagedF32<D, 4, 2>())
+                     : f(PagedF32<D, 4, 4>());
+}
+template <typename T> int paged_ctas(int D, int rows) {
+  auto ctas = [](auto c) { return decltype(c)::CTAS; };
+  return D == 32 ? paged_variant<32>(T(), rows, ctas) : D == 64 ? paged_variant<64>(T(), rows, ctas) : paged_variant<128>(T(), rows, ctas);
 }
 int paged_plan(PagedPlan *pl, const tsfm_kv_pages *p, int B, int M, int n_heads, int max_len, bool weights) {
   if (int rc = pages_shape(p)) return rc;
@@ -98,18 +105,9 @@ int paged_plan(PagedPlan *pl, const tsfm_kv_pages *p, int B, int M, int n_heads,
   if (n_heads % p->n_kv_heads) return TSFM_ERR_SHAPE;
   const long long R = (long long)M * (n_heads / p->n_kv_heads), pairs = (long long)B * p->n_kv_heads;
   if (max_len > kMaxSlots || R > 65535 || pairs > kMaxGridX || (long long)B * M > kMaxGridX) return TSFM_ERR_SHAPE;
-  // rows of a unit: fp32 what a thread's registers hold, bf16 16 to a warp
-  int ctas = PA_F32_CTAS;
-  if (p->dtype == TSFM_BF16) {
-    pl->rows = R <= 8 ? 8 : R <= 16 ? 16 : 32;
-    switch (p->d_head) {
-      case 32: ctas = paged_ctas<32>(pl->rows); break;
-      case 64: ctas = paged_ctas<64>(pl->rows); break;
-      default: ctas = paged_ctas<128>(pl->rows);
-    }
-  } else {
-    pl->rows = R == 1 ? 1 : R == 2 ? 2 : 4;
-  }
+  const bool half = p->dtype == TSFM_BF16;
+  pl->rows = half ? (R <= 8 ? 8 : R <= 16 ? 16 : 32) : R <= 2 ? (int)R : R <= 4 ? 4 : R <= 8 ? 8 : 16;
+  const int ctas = half ? paged_ctas<bf16>(p->d_head, pl->rows) : paged_ctas<float>(p->d_head, pl->rows);
   pl->chunks = (int)((R + pl->rows - 1) / pl->rows);
   if (pairs * pl->chunks > kMaxGridX) return TSFM_ERR_SHAPE;
   const long long tiles = pairs * pl->chunks * ((max_len + PA_TILE - 1) / PA_TILE);
@@ -125,9 +123,9 @@ int paged_plan(PagedPlan *pl, const tsfm_kv_pages *p, int B, int M, int n_heads,
   return TSFM_OK;
 }
 
-// Maps of the pool for TMA: {element, slot, head, page}, boxes of 64 (32) elements and up to 64 slots of a page.  False where
-// the driver has no encoder or refuses the pool's strides.
-bool paged_maps(CUtensorMap *k, CUtensorMap *v, const PagesDev &pg, int D) {
+// Maps of the pool for TMA: {element, slot, head, page}, boxes of 128 (64) bytes and up to 64 slots of a page.  False where the driver
+// has no encoder or refuses the pool's strides.
+bool paged_maps(CUtensorMap *k, CUtensorMap *v, const PagesDev &pg, int D, int e) {
   static const PFN_encodeTiled encode = [] {
     void *fn = nullptr;
     cudaDriverEntryPointQueryResult res{};
@@ -138,43 +136,34 @@ bool paged_maps(CUtensorMap *k, CUtensorMap *v, const PagesDev &pg, int D) {
   const cuuint32_t page = 1u << pg.page_log;
   const cuuint64_t dims[4] = {(cuuint64_t)D, page, (cuuint64_t)pg.n_kv_heads, (cuuint64_t)pg.n_pages};
   const cuuint64_t strides[3] = {(cuuint64_t)pg.slot_stride, (cuuint64_t)pg.head_stride, (cuuint64_t)pg.page_stride};
-  const cuuint32_t box[4] = {(cuuint32_t)std::min(D, 64), std::min(page, 64u), 1, 1}, one[4] = {1, 1, 1, 1};
+  const cuuint32_t box[4] = {(cuuint32_t)std::min(D, 128 / e), std::min(page, 64u), 1, 1}, one[4] = {1, 1, 1, 1};
   for (int i = 0; i < 2; ++i)
-    if (encode(i ? v : k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, i ? pg.v : pg.k, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               D == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    if (encode(i ? v : k, e == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, i ? pg.v : pg.k, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               D * e == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       return false;
   return true;
 }
 
-template <typename C, bool TMA>
-cudaError_t launch_paged_mma(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl, const CUtensorMap &k, const CUtensorMap &v) {
+template <typename C, typename Kernel>
+cudaError_t launch_paged_tiles(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl, const CUtensorMap &k, const CUtensorMap &v, Kernel kernel) {
   // (the attribute belongs to the device's context: set with every call, 0.2 us)
-  if (cudaError_t e = cudaFuncSetAttribute(paged_attn_mma_kernel<C, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES)) return e;
-  paged_attn_mma_kernel<C, TMA><<<pl.grid, C::THREADS, C::SMEM_BYTES, s>>>(a, k, v);
-  return cudaGetLastError();
-}
-template <int D>
-cudaError_t launch_paged_rows(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl, bf16) {
-  CUtensorMap k{}, v{};
-  const bool tma = a.pg.page_log >= 3 && paged_maps(&k, &v, a.pg, D);
-  return paged_variant<D>(pl.rows, [&](auto c) {
-    using C = decltype(c);
-    return tma ? launch_paged_mma<C, true>(s, a, pl, k, v) : launch_paged_mma<C, false>(s, a, pl, k, v);
-  });
-}
-template <int D>
-cudaError_t launch_paged_rows(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl, float) {
-  switch (pl.rows) {
-    case 1: paged_attn_f32_kernel<D, 1><<<pl.grid, PA_THREADS, 0, s>>>(a); break;
-    case 2: paged_attn_f32_kernel<D, 2><<<pl.grid, PA_THREADS, 0, s>>>(a); break;
-    default: paged_attn_f32_kernel<D, 4><<<pl.grid, PA_THREADS, 0, s>>>(a);
-  }
+  if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES)) return e;
+  kernel<<<pl.grid, C::THREADS, C::SMEM_BYTES, s>>>(a, k, v);
   return cudaGetLastError();
 }
 
 template <typename T, int D>
 cudaError_t launch_paged(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl) {
-  if (cudaError_t e = launch_paged_rows<D>(s, a, pl, T())) return e;
+  CUtensorMap k{}, v{};
+  const bool tma = a.pg.page_log >= 3 && paged_maps(&k, &v, a.pg, D, (int)sizeof(T));
+  const cudaError_t err = paged_variant<D>(T(), pl.rows, [&](auto c) {
+    using C = decltype(c);
+    if constexpr (sizeof(T) == 2)
+      return tma ? launch_paged_tiles<C>(s, a, pl, k, v, paged_attn_mma_kernel<C, true>) : launch_paged_tiles<C>(s, a, pl, k, v, paged_attn_mma_kernel<C, false>);
+    else
+      return tma ? launch_paged_tiles<C>(s, a, pl, k, v, paged_attn_f32_kernel<C, true>) : launch_paged_tiles<C>(s, a, pl, k, v, paged_attn_f32_kernel<C, false>);
+  });
+  if (err) return err;
   LAUNCHED();
   // nothing to join where no series has a second tile
   if (a.pg.capacity > PA_TILE && pl.grid > 1) {
