@@ -400,7 +400,8 @@ int tsfm_rope_append(void *stream, const tsfm_rope *rope, const tsfm_kv_pages *p
  *   max_len the longest series of the call in slots, new tokens included: lengths are cut to it.
  *           It sizes the grid and the workspace, not the work.  w_stride >= max_len
  *   workspace  256-byte aligned, tsfm_paged_attention_workspace() bytes; contents do not matter
- * Rows of tokens m >= n_new[b] are not touched.  Results do not depend on the other series' lengths
+ * n_heads is a multiple of n_kv_heads, M n_heads / n_kv_heads at most 65535.  Rows of tokens m >= n_new[b] are not
+ * touched.  Results do not depend on the other series' lengths
  * beyond rounding, and are the same each time for the same call. */
 int tsfm_paged_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int64_t q_stride, void *out, int64_t out_stride,
                          const int32_t *len, const int32_t *n_new, int32_t B, int32_t M, int32_t n_heads, float scale,
@@ -449,7 +450,7 @@ int tsfm_cache_evict(void *stream, const tsfm_kv_pages *pages, const int32_t *ds
  *           has no positive entry)
  *   n_accept [B] int32 out
  *   len, len_out  [B] int32, both or neither: len_out = len + n + 1, the committed length; may be the same
- * K <= TSFM_MAX_K; K = 0 draws one token.  out overlaps no input. */
+ * K <= TSFM_MAX_K, V <= 2^30; K = 0 draws one token.  out overlaps no input. */
 int tsfm_verify_tokens(void *stream, const int32_t *tokens, const float *p, int64_t p_stride, const float *q, int64_t q_stride,
                        int32_t B, int32_t K, int32_t V, const float *u, uint64_t seed, int32_t round_idx, int32_t series0,
                        const int32_t *n_draft, const int32_t *len, int32_t *out, int32_t *n_accept, int32_t *len_out);

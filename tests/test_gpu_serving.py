@@ -218,6 +218,46 @@ def test_attention_split_over_the_length(dtype, D, Hq, Hkv, M, lengths):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D,Hq,Hkv,M,page,lengths", [
+    (64, 4, 2, 1, 512, [700, 3, 512, 1023]), (128, 8, 8, 2, 65536, [900]), (32, 2, 1, 1, 4, [333, 64]), (64, 1, 1, 1, 16, [b % 7 for b in range(3000)]),
+    (128, 96, 2, 1, 32, [500, 64]), (64, 8, 1, 5, 2, [130, 0, 64])])
+def test_attention_over_pages_of_any_size_and_many_series(dtype, D, Hq, Hkv, M, page, lengths):
+    """Pages longer than a tile, of less than a copied box, one that holds everything; thousands of series; more rows than a CTA takes at once."""
+    pool = Pool(len(lengths), Hkv, D, page, [n + M for n in lengths], dtype, seed=6)
+    for b in (0, len(lengths) - 1):
+        stale(pool, b, min(lengths[b] + M, int((pool.table[b] >= 0).sum()) * page - 200) if page > 1000 else lengths[b] + M)
+    check_attention(pool, dtype, Hq, Hkv, D, lengths, [M] * len(lengths), M, weights=len(lengths) < 10)
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    """Calls that overlap on the GPU: each gives what it gives alone."""
+    tsfm = lib()
+    B, Hq, Hkv, D, n = 8, 16, 4, 64, 6000
+    pool = Pool(B, Hkv, D, 32, [n] * B, BF16, seed=12)
+    pages = pool.describe(tsfm)
+    size = tsfm.tsfm_paged_attention_workspace(pages, B, 1, Hq, n)
+    q = [wide((B, 1), Hq * D, BF16, 0, 20 + i) for i in range(2)]
+    length = [ints([n - 500 * b * i for b in range(B)]) for i in (1, 0)]
+    work = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(2)]
+
+    def attend(i, out):
+        tsfm.tsfm_paged_attention(stream(), pages, q[i], Hq * D, out, Hq * D, length[i], None, B, 1, Hq, 0.125, False, 0, n, None, None, None, 0, work[i], size)
+    alone = [torch.empty_like(q[0]) for _ in range(2)]
+    for i in range(2):
+        attend(i, alone[i])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(20):
+        outs = [torch.zeros_like(q[0]) for _ in range(2)]
+        torch.cuda.synchronize()
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                attend(i, outs[i])
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], alone[0]) and torch.equal(outs[1], alone[1])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_attention_with_peaked_and_shifted_scores(dtype):
     """Scores around +-1000 with one slot far above the rest: the running maximum, not the scores' size, sets the range."""
     B, Hkv, D = 3, 2, 64
@@ -374,6 +414,8 @@ def test_evict_long_and_wrong_pages():
     tsfm = lib()
     g = torch.Generator().manual_seed(1)
     check_evict(1, 2, 64, 64, [70001], 30011, 4, 500, BF16, torch.rand(1, 2, 70001, generator=g))
+    check_evict(2, 1, 32, 64, [140001, 5], 1000, 4, 500, BF16, torch.rand(2, 1, 140001, generator=g))         # beyond a cluster's shared memory
+    check_evict(3, 2, 32, 16, [16385, 5000, 8193], 4095, 0, 1, F32, (torch.rand(3, 2, 16385, generator=g) * 50).floor())
     # a wrong page id: what lies there is not moved, the rest is
     pool = Pool(1, 1, 32, 8, [32], F32, seed=2, spare=2)
     table, dst = pool.table.clone(), ints([[pool.spare_ids[0], 99]])
@@ -427,7 +469,7 @@ def distributions(B, K, V, seed, sharp=2.0, apart=0.5, cut=0.0):
 
 
 @pytest.mark.parametrize("B,K,V,cut", [(1, 4, 32003, 0.0), (64, 8, 1000, 0.1), (300, 3, 513, 0.0), (7, 32, 100, 0.1), (3, 5, 100003, 0.0), (40, 2, 16385, 0.2),
-                                       (1, 1, 131072, 0.0), (20, 4, 1, 0.0), (50, 4, 2, 0.0), (9, 4, 31, 0.0), (2, 0, 5000, 0.0), (148, 1, 4097, 0.0)])
+                                       (1, 1, 131072, 0.0), (300, 1, 100003, 0.3), (20, 4, 1, 0.0), (50, 4, 2, 0.0), (9, 4, 31, 0.0), (2, 0, 5000, 0.0), (148, 1, 4097, 0.0)])
 @pytest.mark.parametrize("sampled", [True, False])
 def test_verify_tokens(B, K, V, cut, sampled):
     tokens, p, q, u = distributions(B, K, V, B + V, cut=cut)

@@ -65,7 +65,7 @@ def test_descriptions_of_pages(fn, change, code):
     ("attend", dict(B=0), ARG), ("attend", dict(M=0), ARG), ("attend", dict(heads=0), ARG), ("attend", dict(max_len=0), ARG),
     ("attend", dict(heads=12), SHAPE), ("attend", dict(q=A + 8), SHAPE), ("attend", dict(out=A + 8), SHAPE), ("attend", dict(qs=504), SHAPE),
     ("attend", dict(os=516), SHAPE), ("attend", dict(w_out=A, ws=63), SHAPE), ("attend", dict(work=A + 128), SHAPE), ("attend", dict(bytes=4096), SHAPE),
-    ("attend", dict(max_len=(1 << 30) + 1), SHAPE), ("attend", dict(B=1 << 20, M=1 << 12), SHAPE),
+    ("attend", dict(max_len=(1 << 30) + 1), SHAPE), ("attend", dict(B=1 << 20, M=1 << 12), SHAPE), ("attend", dict(M=65536, B=1), SHAPE),
     ("evict", dict(dst=None), ARG), ("evict", dict(len=None), ARG), ("evict", dict(w=None), ARG), ("evict", dict(kept=None), ARG),
     ("evict", dict(len_out=None), ARG), ("evict", dict(len_out=A), ARG), ("evict", dict(w_out=A), ARG), ("evict", dict(B=0), ARG),
     ("evict", dict(budget=0), ARG), ("evict", dict(sinks=-1), ARG), ("evict", dict(recent=-1), ARG), ("evict", dict(recent=29), ARG),
@@ -73,7 +73,7 @@ def test_descriptions_of_pages(fn, change, code):
     ("evict", dict(dst_stride=-1), SHAPE),
     ("verify", dict(p=None), ARG), ("verify", dict(out=None), ARG), ("verify", dict(n=None), ARG), ("verify", dict(tokens=None), ARG),
     ("verify", dict(B=0), ARG), ("verify", dict(K=-1), ARG), ("verify", dict(K=33), ARG), ("verify", dict(V=0), ARG),
-    ("verify", dict(ps=99), ARG), ("verify", dict(qs=99), ARG), ("verify", dict(len=None), ARG), ("verify", dict(len_out=None), ARG),
+    ("verify", dict(V=(1 << 30) + 1, ps=1 << 31, qs=1 << 31), SHAPE), ("verify", dict(ps=99), ARG), ("verify", dict(qs=99), ARG), ("verify", dict(len=None), ARG), ("verify", dict(len_out=None), ARG),
 ])
 def test_arguments(fn, change, code):
     assert call(fn, **change) == code
