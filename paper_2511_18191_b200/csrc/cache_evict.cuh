@@ -29,10 +29,11 @@ __device__ __forceinline__ uint32_t weight_rank(float w) {
 
 // One CTA, or a cluster of them where it is long, a series and head.  Sinks and recent slots get a rank above all others; then the
 // budget-th largest rank by three rounds of counting, digits of 11, 11 and 10 bits from the top; then the kept slots' places.  A warp
-// owns a contiguous part of the slots, whose ranks stay in shared memory where they fit (16 slots a thread).  Bound: the chain of
-// rounds for one series, instructions for many (32 x 8 heads of up to 16384 slots).  Loops stay loops: with the ranks in
-// registers, hence every pass unrolled, fetching the code took longer than running it.  The counters have copies, by lane: the top
-// digits of a heavy-tailed distribution are few.
+// owns a contiguous part of the slots, whose ranks stay in shared memory where they fit (16 slots a thread).  Loops stay loops: with
+// the ranks in registers, hence every pass unrolled, fetching the code took longer than running it.  The counters have copies, by
+// lane: the top digits of a heavy-tailed distribution are few.
+// Bound: the chain of rounds for one series (4 heads of 4100 slots: 8 us), instructions for many (32 x 8 heads of up to 16384 slots:
+// 32 us).
 constexpr int EVICT_MAX_CLUSTER = 8, EVICT_BINS = 2048;
 
 template <int THREADS> struct EvictShared {

@@ -91,7 +91,7 @@ __device__ __forceinline__ int part_of(const double *part, int n, double target,
 // A cluster of CTAs a series; CTA c, and in it each warp, sums a contiguous part of the row, and keeps the sums of up to 32
 // segments of it.  The draw then falls into a CTA's, a warp's, a segment's part: 256 entries for rows of up to 32 x 256 a warp, which one
 // warp looks through; a longer segment is shared by the CTA's warps as the row was.  Sums are fp64 so that their order decides nothing.
-// Bound: memory, behind the chain proposals - their probabilities - row.  (In place of the segments' sums three more passes over ever
+// Bound: memory, behind the chain proposals - their probabilities - row (256 rows of 100003, 0.8 of the proposals accepted: 43 us, 4.0 TB/s).  (In place of the segments' sums three more passes over ever
 // smaller parts cost 10 us.)
 __global__ void __launch_bounds__(32 * VERIFY_MAX_WARPS, 2) verify_tokens_kernel(VerifyArgs a) {
   namespace cg = cooperative_groups;
