@@ -324,7 +324,7 @@ int tsfm_gemm_bf16_static(void *stream, const void *A, const void *W, float *C,
  * pointers to keys, values, queries and outputs and their strides multiples of 16 bytes. */
 #define TSFM_PAGES_BAD_ID  1
 #define TSFM_PAGES_BAD_LEN 2
-#define TSFM_PAGES_TIMEOUT 4    /* a bounded device-side wait expired: the call's outputs are not to be used */
+#define TSFM_PAGES_TIMEOUT 4    /* a bounded device-side wait expired: outputs that depend on it are NaN */
 
 typedef struct {
   void          *k, *v;         /* dev pools of `dtype`                                         */

@@ -178,6 +178,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_f32_kernel(con
       float2 *ml_scratch = reinterpret_cast<float2 *>(scratch + WARPS * WROWS * D);
 #pragma unroll
       for (int r = 0; r < WROWS; ++r) {
+        if (TMA && sh.dead) l[r] = NAN;
 #pragma unroll
         for (int x = 8; x < 32; x <<= 1) {
           const float om = __shfl_xor_sync(0xffffffffu, m[r], x), ol = __shfl_xor_sync(0xffffffffu, l[r], x);

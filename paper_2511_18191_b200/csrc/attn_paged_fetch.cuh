@@ -50,6 +50,7 @@ template <int S, bool TMA> struct PagedStages {
   unsigned valid[S][2];                            // slots of the tile that exist: in [lo, total), page in the pool
   PagedItem item[S], next[S];                      // of the stages; of the tiles whose page ids are on their way
   int ids[S][TMA ? 8 : PA_TILE];                   // those ids
+  int dead;                                        // a tile did not arrive: what is computed from here on is NaN
 };
 
 // C: D, RB (bytes of a slot's row), PD, PB, PARTS, PART_BYTES, KV_BYTES, ROWS, STAGES, STAGE_BYTES, THREADS.
@@ -76,6 +77,7 @@ __device__ __forceinline__ void paged_fetch(const PagedAttnArgs &a, const PagedR
   const int box_log = TMA ? min(a.pg.page_log, 6) : 0, boxes = PA_TILE >> box_log;
   const uint32_t full0 = smem_u32(sh.full);
   bool dead = false;                             // a tile did not arrive: nothing more is fetched or waited for
+  if (lane == 0) sh.dead = 0;
   if (TMA) {
     if (lane < S) mbar_init(full0 + 8 * lane, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -192,6 +194,7 @@ __device__ __forceinline__ void paged_fetch(const PagedAttnArgs &a, const PagedR
     auto hand_over = [&](int tile) {
       if (TMA && !dead && __any_sync(0xffffffffu, !tile_arrived(full0 + 8 * (tile % S), (tile / S) & 1))) {
         dead = true;
+        if (lane == 0) sh.dead = 1;
         pages_report(a.pg, PAGES_TIMEOUT);
       }
       __threadfence_block();

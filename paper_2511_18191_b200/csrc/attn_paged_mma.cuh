@@ -290,6 +290,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_mma_kernel(con
       for (int q = 0; q < NQ; ++q)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
+          if (TMA && sh.dead) l[q][x] = NAN;
           l[q][x] += __shfl_xor_sync(0xffffffffu, l[q][x], 4);
           l[q][x] += __shfl_xor_sync(0xffffffffu, l[q][x], 8);
           l[q][x] += __shfl_xor_sync(0xffffffffu, l[q][x], 16);

@@ -130,3 +130,16 @@ def test_kv_pages_checks_its_tensors():
                 (k, torch.zeros(4, 16, 2, 64, dtype=torch.bfloat16).transpose(1, 2), t)]:
         with pytest.raises(tsfm.TsfmError):
             tsfm.kv_pages(*bad)
+
+
+def test_a_wait_for_a_tile_that_runs_out_is_reported():
+    """What no GPU that works can show: the one wait on copies sets the status bit, and both kernels turn their sums into NaN."""
+    import os
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2511_18191_b200", "csrc")
+    text = open(os.path.join(csrc, "attn_paged_fetch.cuh")).read()
+    uses = [i for i in range(len(text)) if text.startswith("!tile_arrived(", i)]
+    assert len(uses) == 1
+    after = text[uses[0]:uses[0] + 300]
+    assert "dead = true" in after and "sh.dead = 1" in after and "pages_report(a.pg, PAGES_TIMEOUT)" in after
+    for f in ("attn_paged_mma.cuh", "attn_paged_f32.cuh"):
+        assert "if (TMA && sh.dead)" in open(os.path.join(csrc, f)).read()
