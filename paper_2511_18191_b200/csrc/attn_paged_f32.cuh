@@ -2,7 +2,7 @@
 //
 // WR x WK warps: a warp takes up to 4 query rows against 64 / WK of a tile's slots.  Eight lanes share a slot, a warp works on 8 or 16 at a
 // time, two or four a group of eight lanes, each group with its own running maximum and sum; groups, then warps, are merged when the unit ends.
-// Bound: memory up to 4 rows (64 x 8 heads of 2048 slots of 64: 88 us, 6.1 TB/s; 32 x 8 heads of 4096 slots of 128, 4 rows: 194 us, 5.5 TB/s;
+// Bound: memory up to 4 rows (64 x 8 heads of 2048 slots of 64: 88 us, 6.1 TB/s; 32 x 8 heads of 4096 slots of 128, 4 rows: 180 us, 6.0 TB/s;
 // loads straight into registers 151 and 252), instructions above (64 x 20 heads of 329 slots of 64, 9 rows: 182 us).
 #pragma once
 #include "attn_paged_fetch.cuh"
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_f32_kernel(con
       for (int j = 0; j < N; ++j)
 #pragma unroll
         for (int r = 0; r < WROWS; ++r) sc[j][r] = 0.f;
-#pragma unroll
+#pragma unroll(C::Q_SHARED ? 1 : PARTS)
       for (int p = 0; p < PARTS; ++p) {
         float4 x[N];
 #pragma unroll
