@@ -6,7 +6,7 @@
 // O^T = V^T P^T, P^T by one 8 x 8 transposition per eight slots): rows come in eights, not sixteens, and eight cost half of the
 // instructions and registers.  One more warp fetches (attn_paged_fetch.cuh).  Precision: scores of bf16 operands in fp32;
 // probabilities as two bf16 parts, so that only the result is rounded.
-// Bound: memory up to 16 rows (256 series of up to 8192 slots, 8 heads of 128, 4 rows: 454 us, 6.4 TB/s), the chain of a warp above
+// Bound: memory up to 16 rows (256 series of up to 8192 slots, 8 heads of 128, 4 rows: 443 us, 6.5 TB/s), the chain of a warp above
 // (32 series of up to 16001 slots, 4 heads of 64, 20 rows: 94 us, 3.6 TB/s with the scores that it writes).
 #pragma once
 #include "attn_narrow.cuh"
