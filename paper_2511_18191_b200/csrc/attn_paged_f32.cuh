@@ -12,7 +12,9 @@ namespace tsfm {
 template <int D_, int WROWS_, int WR_> struct PagedF32 {
   static constexpr int D = D_, WROWS = WROWS_, WR = WR_;
   static constexpr int WARPS = D == 128 ? 8 : 4, WK = WARPS / WR, THREADS = 32 * WARPS + 32, KEYS = PA_TILE / WK;
-  static constexpr int ROWS = WROWS * WR, RB = D * 4, N = WROWS == 1 ? 4 : 2;         // N: slots of a group at once
+  static constexpr int ROWS = WROWS * WR, RB = D * 4;
+  static constexpr int N = WROWS == 1 && KEYS >= 16 ? 4 : 2;       // slots of a group at once
+  static_assert(KEYS % (4 * N) == 0, "a warp stays within its slots");
   static constexpr bool Q_SHARED = D == 128 && WROWS == 4;        // four rows of queries beside four of sums would not fit the registers
   static constexpr int PD = 32, PARTS = D / PD, PB = PD * 4, PART_BYTES = PA_TILE * PB;
   static constexpr int KV_BYTES = PA_TILE * RB, Q_BYTES = ROWS * RB;

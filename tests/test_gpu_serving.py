@@ -196,7 +196,8 @@ LENGTHS = [0, 1, 2, 15, 16, 17, 63, 64, 65, 127, 200, 513, 3]
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("D,Hq,Hkv,M,page,order", [
     (64, 8, 8, 1, 16, "heads"), (128, 32, 8, 1, 32, "slots"), (32, 4, 4, 1, 8, "heads"), (64, 20, 4, 9, 16, "heads"), (128, 6, 2, 5, 64, "slots"),
-    (32, 12, 1, 3, 16, "slots"), (64, 3, 3, 33, 1, "heads"), (128, 7, 1, 17, 128, "heads"), (64, 16, 1, 1, 32, "slots"), (64, 34, 2, 1, 32, "slots")])
+    (32, 12, 1, 3, 16, "slots"), (64, 3, 3, 33, 1, "heads"), (128, 7, 1, 17, 128, "heads"), (64, 16, 1, 1, 32, "slots"), (64, 34, 2, 1, 32, "slots"), (128, 3, 3, 1, 16, "heads"), (128, 2, 1, 1, 8, "slots"), (64, 2, 1, 1, 16, "heads"), (32, 4, 2, 1, 32, "heads"),
+    (128, 3, 1, 1, 64, "heads"), (32, 3, 1, 2, 8, "slots"), (128, 8, 1, 1, 16, "heads")])
 @pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 20), (True, 1), (False, 70)])
 def test_attention(dtype, D, Hq, Hkv, M, page, order, causal, window):
     new = [min(M, 1 + b % M) if b % 5 else M for b in range(len(LENGTHS))]
