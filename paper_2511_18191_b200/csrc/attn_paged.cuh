@@ -210,8 +210,9 @@ __global__ void __launch_bounds__(32 * PA_JOIN_WARPS) paged_join_kernel(const __
   }
 }
 
-// w_out = w_in + sum over the rows of 2^(score - lse2); a slot that a row does not see has the score -inf there.  A thread four
-// slots, eight rows of scores in flight.
+// w_out = w_in + sum over the rows of 2^(score - lse2); a slot that a row does not see has the score -inf there and gets nothing from
+// it, whatever lse2 is (NaN where the row's query, or a key that it does see, is not finite).  A thread four slots, eight rows of scores
+// in flight.
 constexpr int PA_WEIGHT_ROWS = 64;
 __global__ void __launch_bounds__(128) paged_weights_kernel(const __grid_constant__ PagedAttnArgs a) {
   __shared__ float s_lse[PA_WEIGHT_ROWS];
@@ -221,15 +222,13 @@ __global__ void __launch_bounds__(128) paged_weights_kernel(const __grid_constan
   const float *w_in = a.w_in ? a.w_in + blockIdx.x * a.w_stride : nullptr;
   float *w_out = a.w_out + blockIdx.x * a.w_stride;
   const int live = s.n_new * a.group;
+  auto weight = [](float score, float lse2) { return score == -INFINITY ? 0.f : exp2f(score - lse2); };
   for (int base = blockIdx.y * 512; base < s.total; base += gridDim.y * 512) {
     const int slot = base + threadIdx.x * 4;
     float w[4] = {0.f, 0.f, 0.f, 0.f};
     for (int r0 = 0; r0 < live; r0 += PA_WEIGHT_ROWS) {
       __syncthreads();
-      if (threadIdx.x < PA_WEIGHT_ROWS) {          // (a row that got nothing gives nothing)
-        const float lse2 = r0 + threadIdx.x < live ? a.lse2[(long long)blockIdx.x * R + r0 + threadIdx.x] : INFINITY;
-        s_lse[threadIdx.x] = lse2 == -INFINITY ? INFINITY : lse2;
-      }
+      if (threadIdx.x < PA_WEIGHT_ROWS && r0 + threadIdx.x < live) s_lse[threadIdx.x] = a.lse2[(long long)blockIdx.x * R + r0 + threadIdx.x];
       __syncthreads();
       if (slot >= s.total || slot < s.tile0 * PA_TILE) continue;       // before the first tile nothing was seen
       const float *src = a.scores + ((long long)blockIdx.x * R + r0) * a.score_stride + slot;
@@ -237,11 +236,11 @@ __global__ void __launch_bounds__(128) paged_weights_kernel(const __grid_constan
       for (int r = 0; r < n; r += 8) {
         float4 v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = r + j < n ? *reinterpret_cast<const float4 *>(src + (r + j) * a.score_stride) : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int j = 0; j < 8; ++j) v[j] = r + j < n ? *reinterpret_cast<const float4 *>(src + (r + j) * a.score_stride) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float lse2 = r + j < n ? s_lse[r + j] : INFINITY;
-          w[0] += exp2f(v[j].x - lse2), w[1] += exp2f(v[j].y - lse2), w[2] += exp2f(v[j].z - lse2), w[3] += exp2f(v[j].w - lse2);
+          const float lse2 = r + j < n ? s_lse[r + j] : 0.f;
+          w[0] += weight(v[j].x, lse2), w[1] += weight(v[j].y, lse2), w[2] += weight(v[j].z, lse2), w[3] += weight(v[j].w, lse2);
         }
       }
     }

@@ -1,0 +1,51 @@
+"""Serving over a cache of pages on the GPU, at the edges of what a call may be given: values that are not finite in the slots or queries
+of some tokens only."""
+import math
+
+import pytest
+import torch
+
+from tests.serving_ref import Pool
+from tests.test_gpu_serving import BF16, F32, ints, lib, stream, wide
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("window", [0, 40])
+@pytest.mark.parametrize("bad", ["query", "nan key", "inf key", "old key"])
+def test_weights_of_slots_that_a_bad_row_does_not_see(dtype, window, bad):
+    """A NaN query, or a key that some tokens see and others do not: out and lse of the rows that do not see it, and the weights of the slots
+    that no row with it sees, are bit for bit those of the call without it; the others are not finite."""
+    tsfm = lib()
+    B, M, Hq, Hkv, D, n = 2, 5, 4, 2, 64, 150
+    pool = Pool(B, Hkv, D, 16, [n + M] * B, dtype, seed=4)
+    q = wide((B, M), Hq * D, dtype, 0, 5)
+    w_in = torch.rand(B, Hkv, n + M, generator=torch.Generator().manual_seed(6)).cuda()
+    pages = pool.describe(tsfm)
+    work = torch.empty(tsfm.tsfm_paged_attention_workspace(pages, B, M, Hq, n + M, True), dtype=torch.uint8, device="cuda")
+    slot = n - 39 if bad == "old key" else n + 2
+    got = []
+    for spoilt in (False, True):
+        if spoilt and bad == "query":
+            q[0, 2, :D] = math.nan                             # token 2, head 0: key head 0
+        elif spoilt:
+            pool.put(pool.k, 0, slot, math.inf if bad == "inf key" else math.nan)
+        out, lse, w = torch.zeros(B, M, Hq * D, dtype=dtype, device="cuda"), torch.zeros(B, M, Hq, device="cuda"), torch.zeros_like(w_in)
+        tsfm.tsfm_paged_attention(stream(), pages, q, q.stride(1), out, out.stride(1), ints([n] * B), None, B, M, Hq, 0.1, True, window, n + M, lse, w_in, w,
+                                  n + M, work, work.numel())
+        got.append((out.cpu().view(B, M, Hq, D), lse.cpu(), w.cpu()))
+    (out0, lse0, w0), (out1, lse1, w1) = got
+    spoilt_row = torch.zeros(B, M, Hq, dtype=torch.bool)
+    spoilt_slot = torch.zeros(B, Hkv, n + M, dtype=torch.bool)
+    for m in range(M):
+        start, end = max(0, n + m + 1 - window) if window else 0, n + m + 1
+        for h in range(Hq):
+            if (m == 2 and h == 0) if bad == "query" else start <= slot < end:
+                spoilt_row[0, m, h] = True
+                spoilt_slot[0, h * Hkv // Hq, start:end] = True
+    assert spoilt_row.any() and not spoilt_slot.all()
+    assert torch.equal(out0[~spoilt_row], out1[~spoilt_row]) and torch.equal(lse0[~spoilt_row], lse1[~spoilt_row])
+    assert not torch.isfinite(out1[spoilt_row]).any() and not torch.isfinite(lse1[spoilt_row]).any()
+    assert torch.equal(w0[~spoilt_slot], w1[~spoilt_slot]) and torch.isfinite(w0).all()
+    assert not torch.isfinite(w1[spoilt_slot]).any()
