@@ -210,38 +210,51 @@ __global__ void __launch_bounds__(32 * PA_JOIN_WARPS) paged_join_kernel(const __
   }
 }
 
-// w_out = w_in + sum over the rows of 2^(score - lse2); a slot that a row does not see has the score -inf there and gets nothing from
-// it, whatever lse2 is (NaN where the row's query, or a key that it does see, is not finite).  A thread four slots, eight rows of scores
-// in flight.
+// w_out = w_in + sum over the rows of 2^(score - lse2); a slot that a row does not see has the score -inf there.  A row whose lse2 is NaN
+// (its query, or a key that it sees, is not finite) gives NaN to the slots that it sees, by their place, and nothing to the others.  A thread
+// four slots, eight rows of scores in flight.
 constexpr int PA_WEIGHT_ROWS = 64;
-__global__ void __launch_bounds__(128) paged_weights_kernel(const __grid_constant__ PagedAttnArgs a) {
+__global__ void __launch_bounds__(128, 7) paged_weights_kernel(const __grid_constant__ PagedAttnArgs a) {
   __shared__ float s_lse[PA_WEIGHT_ROWS];
+  __shared__ unsigned s_nan[2];
+  static_assert(PA_WEIGHT_ROWS == 64, "two warps look them over");
   pdl_wait();
   const int Hkv = a.pg.n_kv_heads, b = blockIdx.x / Hkv, R = a.M * a.group;
   const PagedSpan s = paged_span(a, b, false);
   const float *w_in = a.w_in ? a.w_in + blockIdx.x * a.w_stride : nullptr;
   float *w_out = a.w_out + blockIdx.x * a.w_stride;
   const int live = s.n_new * a.group;
-  auto weight = [](float score, float lse2) { return score == -INFINITY ? 0.f : exp2f(score - lse2); };
   for (int base = blockIdx.y * 512; base < s.total; base += gridDim.y * 512) {
     const int slot = base + threadIdx.x * 4;
     float w[4] = {0.f, 0.f, 0.f, 0.f};
     for (int r0 = 0; r0 < live; r0 += PA_WEIGHT_ROWS) {
       __syncthreads();
-      if (threadIdx.x < PA_WEIGHT_ROWS && r0 + threadIdx.x < live) s_lse[threadIdx.x] = a.lse2[(long long)blockIdx.x * R + r0 + threadIdx.x];
+      if (threadIdx.x < PA_WEIGHT_ROWS) {          // (a row that got nothing gives nothing)
+        const float lse2 = r0 + threadIdx.x < live ? a.lse2[(long long)blockIdx.x * R + r0 + threadIdx.x] : INFINITY;
+        const unsigned bad = __ballot_sync(0xffffffffu, isnan(lse2));
+        if (threadIdx.x % 32 == 0) s_nan[threadIdx.x / 32] = bad;
+        s_lse[threadIdx.x] = lse2 == -INFINITY || isnan(lse2) ? INFINITY : lse2;
+      }
       __syncthreads();
+      unsigned long long nan = s_nan[0] | (unsigned long long)s_nan[1] << 32;
       if (slot >= s.total || slot < s.tile0 * PA_TILE) continue;       // before the first tile nothing was seen
       const float *src = a.scores + ((long long)blockIdx.x * R + r0) * a.score_stride + slot;
       const int n = min(PA_WEIGHT_ROWS, live - r0);
       for (int r = 0; r < n; r += 8) {
         float4 v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = r + j < n ? *reinterpret_cast<const float4 *>(src + (r + j) * a.score_stride) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        for (int j = 0; j < 8; ++j) v[j] = r + j < n ? *reinterpret_cast<const float4 *>(src + (r + j) * a.score_stride) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float lse2 = r + j < n ? s_lse[r + j] : 0.f;
-          w[0] += weight(v[j].x, lse2), w[1] += weight(v[j].y, lse2), w[2] += weight(v[j].z, lse2), w[3] += weight(v[j].w, lse2);
+          const float lse2 = r + j < n ? s_lse[r + j] : INFINITY;
+          w[0] += exp2f(v[j].x - lse2), w[1] += exp2f(v[j].y - lse2), w[2] += exp2f(v[j].z - lse2), w[3] += exp2f(v[j].w - lse2);
         }
+      }
+      for (; nan; nan &= nan - 1) {                // (seldom)
+        const int2 sees = paged_row_range(a, s, token_of(a, r0 + __ffsll(nan) - 1));
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (slot + e >= sees.x && slot + e < sees.y && page_of(a.pg, a.pg.table + (long long)b * a.pg.table_stride, slot + e) >= 0) w[e] = NAN;
       }
     }
 #pragma unroll

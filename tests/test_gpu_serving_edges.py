@@ -49,3 +49,20 @@ def test_weights_of_slots_that_a_bad_row_does_not_see(dtype, window, bad):
     assert not torch.isfinite(out1[spoilt_row]).any() and not torch.isfinite(lse1[spoilt_row]).any()
     assert torch.equal(w0[~spoilt_slot], w1[~spoilt_slot]) and torch.isfinite(w0).all()
     assert not torch.isfinite(w1[spoilt_slot]).any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_bad_row_gives_nothing_to_slots_of_pages_outside_the_pool(dtype):
+    tsfm = lib()
+    Hq, Hkv, D, n = 2, 1, 64, 100
+    pool = Pool(1, Hkv, D, 16, [n], dtype, seed=4)
+    pool.table[0, 3] = pool.k.shape[0]                         # slots 48 to 63
+    q = torch.full((1, 1, Hq * D), math.nan, dtype=dtype, device="cuda")
+    pages = pool.describe(tsfm)
+    work = torch.empty(tsfm.tsfm_paged_attention_workspace(pages, 1, 1, Hq, n, True), dtype=torch.uint8, device="cuda")
+    out, w = torch.zeros_like(q), torch.ones(1, Hkv, n, device="cuda")
+    tsfm.tsfm_paged_attention(stream(), pages, q, Hq * D, out, Hq * D, ints([n]), None, 1, 1, Hq, 0.1, False, 90, n, None, w, w, n, work, work.numel())
+    assert int(pool.status) == tsfm.TSFM_PAGES_BAD_ID
+    hidden = torch.zeros(n, dtype=torch.bool)
+    hidden[:10], hidden[48:64] = True, True                    # before the window; in no page
+    assert (w[0, 0].cpu()[hidden] == 1).all() and w[0, 0].cpu()[~hidden].isnan().all()
