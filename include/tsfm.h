@@ -413,6 +413,12 @@ int tsfm_paged_attention(void *stream, const tsfm_kv_pages *pages, const void *q
 size_t tsfm_paged_attention_workspace(const tsfm_kv_pages *pages, int32_t B, int32_t M, int32_t n_heads, int32_t max_len,
                                       int32_t with_weights);
 
+/* Tests only, process-wide, not to be called while another thread attends: later calls of tsfm_paged_attention wait at most wait_us
+ * (0, or more than the default of 100 ms: the default) for a tile of slots, and with miss_from >= 0 every CTA waits, from that
+ * tile of its own on, for more bytes than it copies: the wait runs out, TSFM_PAGES_TIMEOUT is set, what depends on those tiles
+ * is NaN, and the call ends.  Pages of less than eight slots are copied by other means and do not wait.  (0, -1) restores. */
+void tsfm_debug_tile_wait(int64_t wait_us, int32_t miss_from);
+
 /* Eviction by accumulated weight: per series and key head, the slots to keep become slots 0, 1, .. (in
  * their old order) of the pages that dst_table names, in the same pool.  A series of L = len[b] <=
  * budget slots keeps them all; otherwise the first `sinks`, the last `recent`, and of the slots between

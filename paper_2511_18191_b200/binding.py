@@ -29,7 +29,7 @@ EXPORTS = [
     "tsfm_weights_bytes", "tsfm_weights_offset", "tsfm_weights_bytes_io", "tsfm_weights_offset_io", "tsfm_spec_create", "tsfm_spec_forecast", "tsfm_spec_forecast_variant",
     "tsfm_target_only_forecast", "tsfm_draft_only_forecast", "tsfm_spec_forecast_host", "tsfm_target_only_forecast_host",
     "tsfm_spec_last_trace", "tsfm_accept_round", "tsfm_model_forward", "tsfm_gemm_bf16", "tsfm_gemm_bf16_static",
-    "tsfm_rope_init", "tsfm_rope_append", "tsfm_paged_attention", "tsfm_paged_attention_workspace", "tsfm_cache_evict", "tsfm_verify_tokens",
+    "tsfm_rope_init", "tsfm_rope_append", "tsfm_paged_attention", "tsfm_paged_attention_workspace", "tsfm_debug_tile_wait", "tsfm_cache_evict", "tsfm_verify_tokens",
     "tsfm_spec_debug_guard", "tsfm_spec_set_profiling", "tsfm_spec_kernel_profile", "tsfm_advise_block_size", "tsfm_spec_destroy", "tsfm_launch_count", "tsfm_strerror", "tsfm_last_cuda_error",
 ]
 
@@ -139,6 +139,8 @@ def _load() -> C.CDLL:
     lib.tsfm_paged_attention.argtypes = [vp, pages, vp, i64, vp, i64, vp, vp, i32, i32, i32, f32, i32, i32, i32, vp, vp, vp, i64, vp, sz]
     lib.tsfm_paged_attention_workspace.restype = sz
     lib.tsfm_paged_attention_workspace.argtypes = [pages, i32, i32, i32, i32, i32]
+    lib.tsfm_debug_tile_wait.restype = None
+    lib.tsfm_debug_tile_wait.argtypes = [i64, i32]
     lib.tsfm_cache_evict.restype = C.c_int
     lib.tsfm_cache_evict.argtypes = [vp, pages, vp, i32, vp, vp, i64, i32, i32, i32, i32, i32, vp, vp, i64, vp]
     lib.tsfm_verify_tokens.restype = C.c_int
@@ -371,6 +373,11 @@ def tsfm_paged_attention(stream, pages: tsfm_kv_pages, q, q_stride: int, out, ou
     _check(lib.tsfm_paged_attention(stream, pages, _ptr(q), q_stride, _ptr(out), out_stride, _ptr(len), _ptr(n_new), B, M, n_heads,
                                     scale, causal, window, max_len, _ptr(lse), _ptr(w_in), _ptr(w_out), w_stride, _ptr(workspace),
                                     workspace_bytes), "tsfm_paged_attention")
+
+
+def tsfm_debug_tile_wait(wait_us: int = 0, miss_from: int = -1) -> None:
+    """Tests only: let the attention's wait for a tile run out (no arguments: as it was)."""
+    lib.tsfm_debug_tile_wait(wait_us, miss_from)
 
 
 def tsfm_cache_evict(stream, pages: tsfm_kv_pages, dst_table, dst_stride: int, len, w, w_stride: int, B: int, budget: int, sinks: int,

@@ -39,6 +39,8 @@ struct PagedAttnArgs {
   float *lse2;                                     // [B][heads of keys][M group], with weights only
   float *scores;                                   // [B][heads of keys][M group][score_stride], with weights only
   long long score_stride;
+  unsigned long long wait_ns;                      // limit of a wait for a tile
+  int miss_from;                                   // tests: from this tile of a CTA on more bytes are waited for than are copied
 };
 
 // The token of a query row (row / group).  Rows and groups are below 2^16, so the rounded-up reciprocal is exact.

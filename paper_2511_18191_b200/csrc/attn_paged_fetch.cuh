@@ -5,6 +5,7 @@
 // exchanged as TMA's swizzle does; behind them the queries of a unit's first tile.  TMA copies boxes of up to 64 slots of a page; pages of
 // less than eight slots, and pools that the driver makes no map for, go by cp.async, a slot's row at a time.
 #pragma once
+#include <climits>
 #include "attn_flash.cuh"
 #include "attn_paged.cuh"
 #include "gemm_tc.cuh"
@@ -34,13 +35,13 @@ __device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap *m
       "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
       ::"r"(dst), "l"(map), "r"(x), "r"(slot), "r"(head), "r"(page), "r"(bar) : "memory");
 }
-// Bounded wait for a tile: false if it did not arrive within TC_WAIT_NS.
-__device__ __forceinline__ bool tile_arrived(uint32_t bar, uint32_t parity) {
+// Bounded wait for a tile: false if it did not arrive within `limit` ns.
+__device__ __forceinline__ bool tile_arrived(uint32_t bar, uint32_t parity, unsigned long long limit) {
   unsigned long long t0 = 0;
   for (uint32_t n = 0;; ++n) {
     if (mbar_try_wait(bar, parity)) return true;
     if (n == 256) t0 = globaltimer_ns();
-    if (n > 256 && (n & 255) == 0 && globaltimer_ns() - t0 > TC_WAIT_NS) return false;
+    if (n > 256 && (n & 255) == 0 && globaltimer_ns() - t0 > limit) return false;
   }
 }
 
@@ -76,7 +77,8 @@ __device__ __forceinline__ void paged_fetch(const PagedAttnArgs &a, const PagedR
   // TMA copies boxes of up to 64 slots of one page: a page id a box, else a slot
   const int box_log = TMA ? min(a.pg.page_log, 6) : 0, boxes = PA_TILE >> box_log;
   const uint32_t full0 = smem_u32(sh.full);
-  bool dead = false;                             // a tile did not arrive: nothing more is fetched or waited for
+  bool dead = false;                             // a tile did not arrive: nothing more is fetched
+  int late = 0, issued = INT_MAX;                // (TMA) that tile; the last one that had been asked for by then
   if (lane == 0) sh.dead = 0;
   if (TMA) {
     if (lane < S) mbar_init(full0 + 8 * lane, 1);
@@ -157,7 +159,7 @@ __device__ __forceinline__ void paged_fetch(const PagedAttnArgs &a, const PagedR
     }
     if (TMA) {
       const unsigned ok = __ballot_sync(0xffffffffu, page >= 0) & 0xff;
-      if (lane == 0 && !dead) mbar_expect_tx(full0 + 8 * stage, __popc(ok) * 2 * PARTS * (PB << box_log));
+      if (lane == 0 && !dead) mbar_expect_tx(full0 + 8 * stage, __popc(ok) * 2 * PARTS * (PB << box_log) + (i >= a.miss_from ? 16 : 0));
       __syncwarp();
 #pragma unroll
       for (int i = 0; i < 16 * PARTS; i += 32) {   // (box, part, keys or values)
@@ -192,7 +194,9 @@ __device__ __forceinline__ void paged_fetch(const PagedAttnArgs &a, const PagedR
     }
     flash_commit();
     auto hand_over = [&](int tile) {
-      if (TMA && !dead && __any_sync(0xffffffffu, !tile_arrived(full0 + 8 * (tile % S), (tile / S) & 1))) {
+      // (tiles that were on their way when one did not arrive are waited for too)
+      if (TMA && tile <= issued && __any_sync(0xffffffffu, !tile_arrived(full0 + 8 * (tile % S), (tile / S) & 1, a.wait_ns))) {
+        if (!dead) late = tile, issued = i;
         dead = true;
         if (lane == 0) sh.dead = 1;
         pages_report(a.pg, PAGES_TIMEOUT);
@@ -210,6 +214,9 @@ __device__ __forceinline__ void paged_fetch(const PagedAttnArgs &a, const PagedR
     }
     if (++stage == S) stage = 0;
   }
+  // No copy may land in shared memory that is no longer this CTA's: those that gave no sign get another limit each.
+  if (TMA && dead)
+    for (int tile = late; tile <= issued; ++tile) tile_arrived(full0 + 8 * (tile % S), (tile / S) & 1, a.wait_ns);
 }
 
 }  // namespace tsfm

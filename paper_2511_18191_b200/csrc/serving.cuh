@@ -15,6 +15,10 @@ constexpr int kSms = 148;
 constexpr long long kMaxSlots = 1 << 30;           // of a series: slot arithmetic is 32-bit
 constexpr long long kMaxGridX = 0x7fffffff;
 
+// Limit of a wait for a tile, and the tile of a CTA from which on it runs out (tsfm_debug_tile_wait).
+unsigned long long g_tile_wait_ns = TC_WAIT_NS;
+int g_tile_miss_from = INT_MAX;
+
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 bool stride_ok(int64_t stride, int64_t least, int e) { return stride >= least && stride <= (INT64_MAX >> 4) && stride * e % 16 == 0; }
 
@@ -297,6 +301,8 @@ int tsfm_paged_attention(void *stream, const tsfm_kv_pages *pages, const void *q
   a.lse2 = w_out ? (float *)(ws + pl.lse2) : nullptr;
   a.scores = w_out ? (float *)(ws + pl.scores) : nullptr;
   a.score_stride = pl.score_stride;
+  a.wait_ns = g_tile_wait_ns;
+  a.miss_from = g_tile_miss_from;
   cudaStream_t s = (cudaStream_t)stream;
   cudaError_t err;
   if (pages->dtype == TSFM_BF16)
@@ -305,6 +311,11 @@ int tsfm_paged_attention(void *stream, const tsfm_kv_pages *pages, const void *q
     err = D == 32 ? launch_paged<float, 32>(s, a, pl) : D == 64 ? launch_paged<float, 64>(s, a, pl) : launch_paged<float, 128>(s, a, pl);
   CU_TRY(err);
   return TSFM_OK;
+}
+
+void tsfm_debug_tile_wait(int64_t wait_us, int32_t miss_from) {
+  g_tile_wait_ns = wait_us > 0 ? std::min<unsigned long long>(TC_WAIT_NS, 1000ull * (unsigned long long)std::min<int64_t>(wait_us, 1000000)) : TC_WAIT_NS;
+  g_tile_miss_from = miss_from < 0 ? INT_MAX : miss_from;
 }
 
 int tsfm_cache_evict(void *stream, const tsfm_kv_pages *pages, const int32_t *dst_table, int32_t dst_stride, const int32_t *len,

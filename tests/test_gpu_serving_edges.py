@@ -66,3 +66,43 @@ def test_a_bad_row_gives_nothing_to_slots_of_pages_outside_the_pool(dtype):
     hidden = torch.zeros(n, dtype=torch.bool)
     hidden[:10], hidden[48:64] = True, True                    # before the window; in no page
     assert (w[0, 0].cpu()[hidden] == 1).all() and w[0, 0].cpu()[~hidden].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D,Hq,Hkv,M,page,lengths", [(64, 4, 2, 1, 16, [40] * 1000), (128, 16, 2, 2, 64, [2000, 1, 300]), (32, 20, 1, 2, 8, [500] * 3)])
+@pytest.mark.parametrize("miss_from", [0, 1])
+def test_a_tile_that_does_not_arrive(dtype, D, Hq, Hkv, M, page, lengths, miss_from):
+    """All copies land, but a CTA waits for 16 bytes more from its first or second tile on: the wait ends, the call reports it, what depends on the
+    tile is NaN and the rest is right.  The next call, without it, is as before."""
+    tsfm = lib()
+    B, n = len(lengths), max(lengths) + M
+    pool = Pool(B, Hkv, D, page, [x + M for x in lengths], dtype, seed=3)
+    pages, q = pool.describe(tsfm), wide((B, M), Hq * D, dtype, 0, 8)
+    work = torch.empty(tsfm.tsfm_paged_attention_workspace(pages, B, M, Hq, n, True), dtype=torch.uint8, device="cuda")
+
+    def attend():
+        out, lse = torch.zeros(B, M, Hq * D, dtype=dtype, device="cuda"), torch.zeros(B, M, Hq, device="cuda")
+        w = torch.full((B, Hkv, n), -9.0, device="cuda")
+        tsfm.tsfm_paged_attention(stream(), pages, q, Hq * D, out, Hq * D, ints(lengths), None, B, M, Hq, 0.1, True, 0, n, lse, None, w, n, work, work.numel())
+        torch.cuda.synchronize()
+        status = int(pool.status)
+        pool.status.zero_()
+        return out.cpu().view(B, M, Hq, D), lse.cpu(), w.cpu(), status
+    good = attend()
+    assert good[3] == 0
+    tsfm.tsfm_debug_tile_wait(2000, miss_from)
+    try:
+        bad = attend()
+    finally:
+        tsfm.tsfm_debug_tile_wait()
+    lost = bad[1].isnan()
+    assert torch.equal(bad[0].isnan().all(-1), lost) and torch.equal(bad[0].isnan().any(-1), lost)
+    assert torch.equal(bad[0][~lost], good[0][~lost]) and torch.equal(bad[1][~lost], good[1][~lost])
+    if miss_from == 0:
+        assert bad[3] == tsfm.TSFM_PAGES_TIMEOUT and lost.all()
+        seen = torch.arange(n) < torch.tensor(lengths)[:, None, None] + M
+        assert bad[2][seen.expand_as(bad[2])].isnan().all() and (bad[2][~seen.expand_as(bad[2])] == -9).all()
+    elif B == 1000:                                            # four units a CTA, the first one whole
+        assert bad[3] == tsfm.TSFM_PAGES_TIMEOUT and lost.any() and not lost.all()
+    again = attend()
+    assert again[3] == 0 and all(torch.equal(x, y) for x, y in zip(again[:3], good[:3]))
