@@ -309,7 +309,7 @@ int tsfm_gemm_bf16_static(void *stream, const void *A, const void *W, float *C,
  * All four enqueue kernels on `stream` and return; they allocate nothing, keep nothing between
  * calls, and can be captured into a CUDA graph.  Pointers are dev on the current device unless
  * said otherwise; `stream` belongs to the current device.  Two calls that overlap on the GPU must
- * not share a workspace, nor pages that one of them writes.
+ * not share a workspace, nor pages, lengths or counts of tokens that one of them writes.
  *
  * A pool holds pages of page_size slots for all series.  Slot s of series b lies in page
  * table[b * table_stride + s / page_size]; element i of its key for head h is

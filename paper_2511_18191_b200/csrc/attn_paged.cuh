@@ -73,6 +73,22 @@ __device__ __forceinline__ int2 paged_row_range(const PagedAttnArgs &a, const Pa
   return make_int2(a.window ? max(0, end - a.window) : 0, end);
 }
 
+// The tile after (b, u, t) in a run, next() the span of the series after b's last one.  Bounded by B and units: should a length change under
+// a call, which nobody may let happen, the walk stays at the last series and the call ends.
+#pragma nv_exec_check_disable
+template <typename F>
+__host__ __device__ __forceinline__ void paged_next_tile(int &b, int &u, int &t, PagedSpan &sp, int B, int units, F next) {
+  if (++t < sp.tiles) return;
+  t = 0;
+  if (++u < units) return;
+  u = 0;
+  while (b + 1 < B) {
+    ++b;
+    sp = next();
+    if (sp.tiles) break;
+  }
+}
+
 // The CTA's run of tiles: `count` of them from tile `first` of unit `u` of series `b`; per: tiles a CTA; unit0: number of that
 // unit's first tile.
 struct PagedRun {

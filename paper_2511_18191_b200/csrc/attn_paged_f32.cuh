@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_f32_kernel(con
     PagedMeta meta{-1, 0, 0, 0};
     if (run.count > 0 && run.first) {
       const int tiles = paged_span(a, run.b, false).tiles;
-      meta = PagedMeta{run.b, run.u, (int)(run.unit0 / run.per), (int)((run.unit0 + tiles - 1) / run.per)};
+      meta = PagedMeta{run.b, run.u, (int)(run.unit0 / run.per), (int)min((run.unit0 + tiles - 1) / run.per, (long long)gridDim.x - 1)};
     }
     a.meta[blockIdx.x] = meta;
   }

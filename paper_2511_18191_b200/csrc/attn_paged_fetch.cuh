@@ -98,17 +98,11 @@ __device__ __forceinline__ void paged_fetch(const PagedAttnArgs &a, const PagedR
     }
     if (lane == 0) sh.next[ring] = PagedItem{b, u, t, ni == 0 || t == 0, sp};
     if (++ni == run.count) return;
-    if (++t == sp.tiles) {
-      t = 0;
-      if (++u == a.units) {
-        u = 0;
-        do {                                     // (there is one: the run goes on)
-          ++b;
-          sp = paged_span_of(a, len_next, new_next, false);
-          fetch_next();
-        } while (sp.tiles == 0);
-      }
-    }
+    paged_next_tile(b, u, t, sp, a.B, a.units, [&]() {
+      const PagedSpan at = paged_span_of(a, len_next, new_next, false);
+      fetch_next();
+      return at;
+    });
   };
   for (int j = 0; j < AHEAD; ++j) fetch_ids();
   flash_commit();

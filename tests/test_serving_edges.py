@@ -1,0 +1,54 @@
+"""Serving over a cache of pages, at the edges of what a call may be given: what needs no GPU."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+WALK = r"""
+#include <cstdio>
+#include <vector>
+#include "attn_paged.cuh"
+using namespace tsfm;
+// The walk from tile `first` of series b0 over `count` tiles; spans as they are now, `later` as they are once the walk has begun.
+static int walk(const std::vector<int> &now, const std::vector<int> &later, int units, int b0, int count, bool print) {
+  int b = b0, u = 0, t = 0, calls = 0;
+  PagedSpan sp{};
+  sp.tiles = now[b];
+  for (int i = 0; i < count; ++i) {
+    if (print) std::printf("%d %d %d\n", b, u, t);
+    if (b < 0 || b >= (int)now.size() || u < 0 || u >= units || t < 0 || calls > (int)now.size()) return 1;
+    if (i + 1 < count)
+      paged_next_tile(b, u, t, sp, (int)now.size(), units, [&]() {
+        ++calls;
+        PagedSpan s{};
+        s.tiles = later[b];
+        return s;
+      });
+  }
+  return 0;
+}
+int main() {
+  const std::vector<int> lengths = {0, 2, 0, 0, 1, 3, 0}, none(7, 0), long_ones(7, 1 << 20);
+  if (walk(lengths, lengths, 2, 1, 2 * (2 + 1 + 3), true)) return 2;
+  for (int b0 : {1, 4, 5})
+    for (const auto &later : {none, long_ones, std::vector<int>{0, 0, 0, 1, 0, 0, 0}})
+      if (walk(lengths, later, 2, b0, 1000, false)) return 3;
+  return 0;
+}
+"""
+
+
+@pytest.mark.skipif(shutil.which(os.environ.get("NVCC", "nvcc")) is None, reason="no nvcc")
+def test_the_walk_over_tiles_ends_whatever_lengths_become(tmp_path):
+    """Every unit's tiles in order, empty series left out; and where lengths are others than at the start (a call that overlaps another one
+    that writes them), no more steps than series, and no index outside."""
+    src, exe = tmp_path / "walk.cu", tmp_path / "walk"
+    src.write_text(WALK)
+    subprocess.run([os.environ.get("NVCC", "nvcc"), "-std=c++17", "-O1", "-gencode", "arch=compute_100a,code=sm_100a", "-I", os.path.join(ROOT, "include"),
+                    "-I", os.path.join(ROOT, "paper_2511_18191_b200", "csrc"), "-o", str(exe), str(src)], check=True)
+    run = subprocess.run([str(exe)], capture_output=True, text=True, timeout=60)
+    want = [(b, u, t) for b, n in ((1, 2), (4, 1), (5, 3)) for u in range(2) for t in range(n)]
+    assert run.returncode == 0 and [tuple(map(int, x.split())) for x in run.stdout.splitlines()] == want
