@@ -379,7 +379,7 @@ int tsfm_rope_init(tsfm_rope *rope, int32_t layout, int32_t rot_dim, int32_t sca
  *   pos     [B] position of the first new token; NULL: len (they part once slots are evicted)
  *   len     [B] slots already in the cache
  *   n_new   [B] new tokens, cut to 0 .. M; NULL: M each.  Rows behind them are not touched
- * rope->rot_dim <= d_head; n_heads >= 0.  Pages that are written belong to one series only. */
+ * rope->rot_dim <= d_head; n_heads >= 0; a row of at most 2^30 elements.  Pages that are written belong to one series only. */
 int tsfm_rope_append(void *stream, const tsfm_rope *rope, const tsfm_kv_pages *pages, const void *qkv, int64_t qkv_stride,
                      void *q_out, int64_t q_out_stride, const int32_t *pos, const int32_t *len, const int32_t *n_new,
                      int32_t B, int32_t M, int32_t n_heads);

@@ -228,7 +228,7 @@ int tsfm_rope_append(void *stream, const tsfm_rope *rope, const tsfm_kv_pages *p
   if (int rc = pages_init(&a.pg, pages)) return rc;
   const int D = pages->d_head, e = (int)elt_bytes(pages->dtype);
   const int64_t row = ((int64_t)n_heads + 2ll * pages->n_kv_heads) * D;
-  if (rope->rot_dim > D || (int64_t)B * M > kMaxGridX) return TSFM_ERR_SHAPE;
+  if (rope->rot_dim > D || (int64_t)B * M > kMaxGridX || row > 1 << 30) return TSFM_ERR_SHAPE;       // (elements of a row are counted in 32 bits)
   if (!aligned16(qkv) || !stride_ok(qkv_stride, row, e)) return TSFM_ERR_SHAPE;
   if (q_out && (!aligned16(q_out) || !stride_ok(q_out_stride, (int64_t)n_heads * D, e))) return TSFM_ERR_SHAPE;
   if (q_out == qkv && q_out_stride != qkv_stride) return TSFM_ERR_ARG;

@@ -5,6 +5,9 @@ import subprocess
 
 import pytest
 
+import paper_2511_18191_b200 as tsfm
+from tests.test_serving_refusals import SHAPE, call, pages
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 WALK = r"""
@@ -52,3 +55,11 @@ def test_the_walk_over_tiles_ends_whatever_lengths_become(tmp_path):
     run = subprocess.run([str(exe)], capture_output=True, text=True, timeout=60)
     want = [(b, u, t) for b, n in ((1, 2), (4, 1), (5, 3)) for u in range(2) for t in range(n)]
     assert run.returncode == 0 and [tuple(map(int, x.split())) for x in run.stdout.splitlines()] == want
+
+
+@pytest.mark.parametrize("dtype", [tsfm.TSFM_F32, tsfm.TSFM_BF16])
+@pytest.mark.parametrize("heads,kv", [(1 << 25, 8), (1 << 24, 8), (8, 1 << 24), (2 ** 31 - 1, 8), (0, 2 ** 31 - 1)])
+def test_rows_of_an_append_stay_below_32_bits(dtype, heads, kv):
+    """2^25 heads of 64 are 2^31 elements: their places within a row would not fit the kernels' 32-bit offsets (the limit is half of that, so that
+    no loop over a row passes them either)."""
+    assert call("append", pages=pages(dtype=dtype, n_kv_heads=kv), heads=heads, qs=1 << 40, q_out=None) == SHAPE
