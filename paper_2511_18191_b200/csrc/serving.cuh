@@ -14,6 +14,7 @@ namespace {
 constexpr int kSms = 148;
 constexpr long long kMaxSlots = 1 << 30;           // of a series: slot arithmetic is 32-bit
 constexpr long long kMaxGridX = 0x7fffffff;
+constexpr long long kMaxScores = 1ll << 48;        // of a workspace: far above any memory, far below what its size in bytes can say
 
 // Limit of a wait for a tile, and the tile of a CTA from which on it runs out (tsfm_debug_tile_wait).
 unsigned long long g_tile_wait_ns = TC_WAIT_NS;
@@ -121,6 +122,7 @@ int paged_plan(PagedPlan *pl, const tsfm_kv_pages *p, int B, int M, int n_heads,
   pl->part_ml = take(sizeof(float2) * 2 * pl->grid * pl->rows);
   pl->part_o = take(sizeof(float) * 2 * pl->grid * pl->rows * p->d_head);
   pl->score_stride = ((long long)max_len + 31) / 32 * 32;
+  if (weights && pairs * R > kMaxScores / pl->score_stride) return TSFM_ERR_SHAPE;
   pl->lse2 = weights ? take(sizeof(float) * pairs * R) : 0;
   pl->scores = weights ? take(sizeof(float) * pairs * R * pl->score_stride) : 0;
   pl->bytes = at;

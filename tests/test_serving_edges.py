@@ -6,7 +6,7 @@ import subprocess
 import pytest
 
 import paper_2511_18191_b200 as tsfm
-from tests.test_serving_refusals import SHAPE, call, pages
+from tests.test_serving_refusals import A, SHAPE, call, pages
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -63,3 +63,12 @@ def test_rows_of_an_append_stay_below_32_bits(dtype, heads, kv):
     """2^25 heads of 64 are 2^31 elements: their places within a row would not fit the kernels' 32-bit offsets (the limit is half of that, so that
     no loop over a row passes them either)."""
     assert call("append", pages=pages(dtype=dtype, n_kv_heads=kv), heads=heads, qs=1 << 40, q_out=None) == SHAPE
+
+
+@pytest.mark.parametrize("B,M,heads,max_len", [(1 << 20, 2047, 32, 1 << 30), (1 << 16, 1000, 64, 1 << 30), (1 << 20, 1, 8, 1 << 30)])
+def test_workspaces_that_no_memory_holds(B, M, heads, max_len):
+    """The scores of these shapes take 2^64 bytes and more (the size would come out small), or 2^55."""
+    kv = pages(n_kv_heads=1)
+    assert tsfm.tsfm_paged_attention_workspace(kv, B, M, heads, max_len, True) == 0
+    assert tsfm.tsfm_paged_attention_workspace(kv, B, M, heads, max_len, False) > 0       # without weights there are none
+    assert call("attend", pages=kv, B=B, M=M, heads=heads, max_len=max_len, w_out=A, ws=max_len, qs=heads * 64, os=heads * 64, bytes=2 ** 64 - 1) == SHAPE
