@@ -387,7 +387,7 @@ int tsfm_rope_append(void *stream, const tsfm_rope *rope, const tsfm_kv_pages *p
 /* Attention of up to M new tokens per series over the cache.  Token m < n_new[b], head h, reads key
  * head h / (n_heads / n_kv_heads); it sees slots max(0, end - window) <= s < end, where end is
  * len[b] + m + 1 with `causal` (the new tokens are in the cache, each sees those before it and
- * itself) and len[b] without (they are not; encoder caches).  window 0: no lower bound.
+ * itself) and len[b] without (they are not; encoder caches).  window 0: no lower bound.  |scale| < 2.3e38.
  *   out  softmax(scale q.k) v in fp32, rounded once;  lse  log of the sum of exp(scale q.k).
  * A token that sees nothing (or only scores of -inf) gets out 0, lse -inf.  What lies in slots that a
  * token does not see has no influence, NaN included.

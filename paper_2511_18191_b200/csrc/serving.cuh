@@ -20,6 +20,7 @@ constexpr long long kMaxScores = 1ll << 48;        // of a workspace: far above 
 unsigned long long g_tile_wait_ns = TC_WAIT_NS;
 int g_tile_miss_from = INT_MAX;
 
+constexpr float kLog2E = 1.4426950408889634f;      // scores are kept in base 2
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 bool stride_ok(int64_t stride, int64_t least, int e) { return stride >= least && stride <= (INT64_MAX >> 4) && stride * e % 16 == 0; }
 
@@ -265,7 +266,7 @@ int tsfm_paged_attention(void *stream, const tsfm_kv_pages *pages, const void *q
                          const int32_t *len, const int32_t *n_new, int32_t B, int32_t M, int32_t n_heads, float scale,
                          int32_t causal, int32_t window, int32_t max_len, float *lse, const float *w_in, float *w_out,
                          int64_t w_stride, void *workspace, size_t workspace_bytes) {
-  if (!q || !out || !len || !workspace || window < 0 || !std::isfinite(scale) || (w_in && !w_out)) return TSFM_ERR_ARG;
+  if (!q || !out || !len || !workspace || window < 0 || !std::isfinite(scale * kLog2E) || (w_in && !w_out)) return TSFM_ERR_ARG;
   PagedPlan pl;
   if (int rc = paged_plan(&pl, pages, B, M, n_heads, max_len, w_out != nullptr)) return rc;
   PagedAttnArgs a{};
@@ -287,7 +288,7 @@ int tsfm_paged_attention(void *stream, const tsfm_kv_pages *pages, const void *q
   a.n_heads = n_heads;
   a.group = n_heads / pages->n_kv_heads;
   a.group_magic = (uint32_t)(((1ull << 32) + a.group - 1) / a.group);
-  a.scale2 = scale * 1.4426950408889634f;
+  a.scale2 = scale * kLog2E;
   a.causal = causal != 0;
   a.window = window;
   a.lse = lse;

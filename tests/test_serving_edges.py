@@ -6,7 +6,7 @@ import subprocess
 import pytest
 
 import paper_2511_18191_b200 as tsfm
-from tests.test_serving_refusals import A, SHAPE, call, pages
+from tests.test_serving_refusals import A, ARG, SHAPE, call, pages
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -72,3 +72,9 @@ def test_workspaces_that_no_memory_holds(B, M, heads, max_len):
     assert tsfm.tsfm_paged_attention_workspace(kv, B, M, heads, max_len, True) == 0
     assert tsfm.tsfm_paged_attention_workspace(kv, B, M, heads, max_len, False) > 0       # without weights there are none
     assert call("attend", pages=kv, B=B, M=M, heads=heads, max_len=max_len, w_out=A, ws=max_len, qs=heads * 64, os=heads * 64, bytes=2 ** 64 - 1) == SHAPE
+
+
+@pytest.mark.parametrize("scale", [2.4e38, -2.4e38, 3.4e38])
+def test_a_scale_that_base_2_does_not_hold(scale):
+    """scale * log2(e) beyond the largest float: a score of 0 would become 0 x inf."""
+    assert call("attend", scale=scale) == ARG
