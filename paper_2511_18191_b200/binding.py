@@ -85,6 +85,7 @@ class tsfm_kv_pages(C.Structure):
                 ("table", C.c_void_p), ("table_stride", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int32),
                 ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32), ("dtype", C.c_int32),
                 ("status", C.c_void_p)]
+    device = rows = None                       # of the tensors, where kv_pages has made the description
 
 
 class tsfm_rope(C.Structure):
@@ -335,6 +336,18 @@ def tsfm_gemm_bf16_static(stream, A, W, Cout, M: int, N: int, Kd: int) -> None:
 
 
 # ---------------------------------------------------------------- serving over a cache of pages
+_I32 = _F32 = _current_device = None            # torch's, once a tensor has come in
+_ELEMENT: Dict[int, object] = {}
+
+
+def _torch_names() -> None:
+    global _I32, _F32, _current_device
+    import torch
+    _ELEMENT.update({TSFM_F32: torch.float32, TSFM_BF16: torch.bfloat16})
+    _F32, _current_device = torch.float32, torch._C._cuda_getDevice        # (asked only with a tensor of a GPU at hand)
+    _I32 = torch.int32                         # (last: it says that the others are there)
+
+
 def kv_pages(k, v, table, status=None) -> tsfm_kv_pages:
     """Describe a pool: k, v [n_pages, n_kv_heads, page_size, d_head] tensors of one dtype and the same strides (a pool laid out
     [n_pages, page_size, n_kv_heads, d_head] goes in as k.transpose(1, 2)), table [B, max_pages] int32.  The tensors stay the
@@ -345,8 +358,52 @@ def kv_pages(k, v, table, status=None) -> tsfm_kv_pages:
             or table.dim() != 2 or table.dtype != torch.int32 or table.stride(1) != 1 or len({k.device, v.device, table.device}) != 1
             or (status is not None and (status.dtype != torch.int32 or status.device != k.device))):
         raise TsfmError(TSFM_ERR_ARG, "kv_pages")
-    return tsfm_kv_pages(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), table.data_ptr(), table.stride(0),
-                         table.shape[1], k.shape[0], k.shape[2], k.shape[1], k.shape[3], code, _ptr(status))
+    pages = tsfm_kv_pages(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), table.data_ptr(), table.stride(0),
+                          table.shape[1], k.shape[0], k.shape[2], k.shape[1], k.shape[3], code, _ptr(status))
+    pages.device, pages.rows = k.get_device(), table.shape[0]
+    return pages
+
+
+# The calls below take tensors on the current device, of the types that include/tsfm.h names; what would be read as something else is
+# TSFM_ERR_ARG: another type, a host tensor or array, another device, a vector that is not contiguous, a table of fewer rows than series.
+# (0.2 us a tensor: 0.8 to 1.5 us a call; the library itself takes addresses.)
+def _device_of(t, where: str, pages=None, B: int = 0) -> int:
+    """The device of the tensor that a call cannot do without."""
+    if _I32 is None:
+        _torch_names()
+    device = -1 if t is None or isinstance(t, np.ndarray) else t.get_device()
+    if device < 0 or device != _current_device():
+        raise TsfmError(TSFM_ERR_ARG, where)
+    if pages is not None and pages.device is not None and (pages.device != device or pages.rows < B):
+        raise TsfmError(TSFM_ERR_ARG, where)
+    return device
+
+
+def _rows(t, dtype, device: int, where: str) -> Optional[int]:
+    """Address of a tensor whose row stride the caller gives (None -> NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != device:
+        raise TsfmError(TSFM_ERR_ARG, where)
+    return t.data_ptr()
+
+
+def _dense(t, dtype, device: int, where: str) -> Optional[int]:
+    """Address of a contiguous tensor (None -> NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        raise TsfmError(TSFM_ERR_ARG, where)
+    return t.data_ptr()
+
+
+def _bytes(t, device: int, where: str) -> Optional[int]:
+    """Address of a contiguous tensor of any type (None -> NULL)."""
+    if t is None:
+        return None
+    if isinstance(t, np.ndarray) or t.get_device() != device or not t.is_contiguous():
+        raise TsfmError(TSFM_ERR_ARG, where)
+    return t.data_ptr()
 
 
 def tsfm_rope_init(layout: int, rot_dim: int, scaling: int, base: float, factor: float = 1.0, original_len: float = 0.0,
@@ -359,8 +416,11 @@ def tsfm_rope_init(layout: int, rot_dim: int, scaling: int, base: float, factor:
 
 def tsfm_rope_append(stream, rope: tsfm_rope, pages: tsfm_kv_pages, qkv, qkv_stride: int, q_out, q_out_stride: int, pos, len, n_new,
                      B: int, M: int, n_heads: int) -> None:
-    _check(lib.tsfm_rope_append(stream, rope, pages, _ptr(qkv), qkv_stride, _ptr(q_out), q_out_stride, _ptr(pos), _ptr(len),
-                                _ptr(n_new), B, M, n_heads), "tsfm_rope_append")
+    me = "tsfm_rope_append"
+    d = _device_of(len, me, pages, B)
+    e = _ELEMENT.get(pages.dtype)
+    _check(lib.tsfm_rope_append(stream, rope, pages, _rows(qkv, e, d, me), qkv_stride, _rows(q_out, e, d, me), q_out_stride,
+                                _dense(pos, _I32, d, me), _dense(len, _I32, d, me), _dense(n_new, _I32, d, me), B, M, n_heads), me)
 
 
 def tsfm_paged_attention_workspace(pages: tsfm_kv_pages, B: int, M: int, n_heads: int, max_len: int, with_weights: bool = False) -> int:
@@ -370,9 +430,13 @@ def tsfm_paged_attention_workspace(pages: tsfm_kv_pages, B: int, M: int, n_heads
 def tsfm_paged_attention(stream, pages: tsfm_kv_pages, q, q_stride: int, out, out_stride: int, len, n_new, B: int, M: int, n_heads: int,
                          scale: float, causal: bool, window: int, max_len: int, lse, w_in, w_out, w_stride: int, workspace,
                          workspace_bytes: int) -> None:
-    _check(lib.tsfm_paged_attention(stream, pages, _ptr(q), q_stride, _ptr(out), out_stride, _ptr(len), _ptr(n_new), B, M, n_heads,
-                                    scale, causal, window, max_len, _ptr(lse), _ptr(w_in), _ptr(w_out), w_stride, _ptr(workspace),
-                                    workspace_bytes), "tsfm_paged_attention")
+    me = "tsfm_paged_attention"
+    d = _device_of(len, me, pages, B)
+    e = _ELEMENT.get(pages.dtype)
+    _check(lib.tsfm_paged_attention(stream, pages, _rows(q, e, d, me), q_stride, _rows(out, e, d, me), out_stride, _dense(len, _I32, d, me),
+                                    _dense(n_new, _I32, d, me), B, M, n_heads, scale, causal, window, max_len, _dense(lse, _F32, d, me),
+                                    _rows(w_in, _F32, d, me), _rows(w_out, _F32, d, me), w_stride,
+                                    _bytes(workspace, d, me), workspace_bytes), me)
 
 
 def tsfm_debug_tile_wait(wait_us: int = 0, miss_from: int = -1) -> None:
@@ -382,15 +446,20 @@ def tsfm_debug_tile_wait(wait_us: int = 0, miss_from: int = -1) -> None:
 
 def tsfm_cache_evict(stream, pages: tsfm_kv_pages, dst_table, dst_stride: int, len, w, w_stride: int, B: int, budget: int, sinks: int,
                      recent: int, max_len: int, kept, w_out, w_out_stride: int, len_out) -> None:
-    _check(lib.tsfm_cache_evict(stream, pages, _ptr(dst_table), dst_stride, _ptr(len), _ptr(w), w_stride, B, budget, sinks, recent,
-                                max_len, _ptr(kept), _ptr(w_out), w_out_stride, _ptr(len_out)), "tsfm_cache_evict")
+    me = "tsfm_cache_evict"
+    d = _device_of(len, me, pages, B)
+    _check(lib.tsfm_cache_evict(stream, pages, _rows(dst_table, _I32, d, me), dst_stride, _dense(len, _I32, d, me), _rows(w, _F32, d, me), w_stride,
+                                B, budget, sinks, recent, max_len, _dense(kept, _I32, d, me), _rows(w_out, _F32, d, me), w_out_stride,
+                                _dense(len_out, _I32, d, me)), me)
 
 
 def tsfm_verify_tokens(stream, tokens, p, p_stride: int, q, q_stride: int, B: int, K: int, V: int, u, seed: int, round_idx: int,
                        series0: int, n_draft, len, out, n_accept, len_out) -> None:
-    _check(lib.tsfm_verify_tokens(stream, _ptr(tokens), _ptr(p), p_stride, _ptr(q), q_stride, B, K, V, _ptr(u), seed, round_idx,
-                                  series0, _ptr(n_draft), _ptr(len), _ptr(out), _ptr(n_accept), _ptr(len_out)),
-           "tsfm_verify_tokens")
+    me = "tsfm_verify_tokens"
+    d = _device_of(p, me)
+    _check(lib.tsfm_verify_tokens(stream, _dense(tokens, _I32, d, me), _rows(p, _F32, d, me), p_stride, _rows(q, _F32, d, me), q_stride, B, K, V,
+                                  _dense(u, _F32, d, me), seed, round_idx, series0, _dense(n_draft, _I32, d, me), _dense(len, _I32, d, me),
+                                  _dense(out, _I32, d, me), _dense(n_accept, _I32, d, me), _dense(len_out, _I32, d, me)), me)
 
 
 def tsfm_spec_debug_guard(h, region: int = -1, damage: bool = False) -> int:
