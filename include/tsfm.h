@@ -306,6 +306,9 @@ int tsfm_gemm_bf16_static(void *stream, const void *A, const void *W, float *C,
  * moves: the round's tokens lie in slots len[b] .. len[b] + n_new[b] - 1, and what a verification
  * rejects is garbage behind the new length.
  *
+ * A decoder handle does not use these calls, and its norms, MLPs, embeddings and heads are not exported as steps
+ * of their own: what lies between an append and a verification is the caller's (tsfm_gemm_bf16 is there for products).
+ *
  * All four enqueue kernels on `stream` and return; they allocate nothing, keep nothing between
  * calls, and can be captured into a CUDA graph.  Pointers are dev on the current device unless
  * said otherwise; `stream` belongs to the current device.  Two calls that overlap on the GPU must
@@ -318,7 +321,8 @@ int tsfm_gemm_bf16_static(void *stream, const void *A, const void *W, float *C,
  * only.  Device data that is wrong does not fault: an id outside [0, n_pages) is never
  * followed (its slots are hidden from attention, appends to it are dropped, an eviction copies
  * nothing from or to it) and sets TSFM_PAGES_BAD_ID in *status; a length below 0 or beyond the
- * capacity is cut to it and sets TSFM_PAGES_BAD_LEN.  *status is only ever OR-ed into.
+ * capacity is cut to it (an append drops the tokens that lie outside) and sets TSFM_PAGES_BAD_LEN.
+ * *status is only ever OR-ed into.
  *
  * Restrictions (TSFM_ERR_SHAPE): d_head 32, 64 or 128; page_size a power of two up to 65536;
  * pointers to keys, values, queries and outputs and their strides multiples of 16 bytes. */
@@ -377,7 +381,8 @@ int tsfm_rope_init(tsfm_rope *rope, int32_t layout, int32_t rot_dim, int32_t sca
  *   q_out   [B, M] rows of n_heads * d_head, q_out_stride apart: turned queries.  May be qkv itself
  *           (same stride: in place), otherwise disjoint from it; NULL: queries are not touched
  *   pos     [B] position of the first new token; NULL: len (they part once slots are evicted)
- *   len     [B] slots already in the cache
+ *   len     [B] slots already in the cache; not cut here: a token whose slot is below 0 or beyond the capacity is not
+ *           appended (its queries are turned all the same) and sets TSFM_PAGES_BAD_LEN
  *   n_new   [B] new tokens, cut to 0 .. M; NULL: M each.  Rows behind them are not touched
  * rope->rot_dim <= d_head; n_heads >= 0; a row of at most 2^30 elements.  Pages that are written belong to one series only. */
 int tsfm_rope_append(void *stream, const tsfm_rope *rope, const tsfm_kv_pages *pages, const void *qkv, int64_t qkv_stride,
@@ -388,9 +393,12 @@ int tsfm_rope_append(void *stream, const tsfm_rope *rope, const tsfm_kv_pages *p
  * head h / (n_heads / n_kv_heads); it sees slots max(0, end - window) <= s < end, where end is
  * len[b] + m + 1 with `causal` (the new tokens are in the cache, each sees those before it and
  * itself) and len[b] without (they are not; encoder caches).  window 0: no lower bound.  |scale| < 2.3e38.
- *   out  softmax(scale q.k) v in fp32, rounded once;  lse  log of the sum of exp(scale q.k).
+ *   out  softmax(scale q.k) v;  lse  log of the sum of exp(scale q.k).
+ * Scores, maxima and sums are fp32 and out is rounded once.  With bf16 the probabilities enter the product with the
+ * values as two bf16 parts: 2^-16 of each probability is lost, not 2^-8.  lse and w_out are fp32 throughout.
  * A token that sees nothing (or only scores of -inf) gets out 0, lse -inf.  What lies in slots that a
- * token does not see has no influence, NaN included.
+ * token does not see has no influence, NaN included.  A query, or a key or value in a slot that a token sees, that is not
+ * finite makes the outputs that it enters not finite; whether NaN or infinite is not specified.
  *   q, out  [B, M] rows of n_heads * d_head, q_stride / out_stride elements apart
  *   lse     [B, M, n_heads] fp32, nullable
  *   w_out   nullable, [B, n_kv_heads] rows of w_stride fp32: w_out = w_in + the probabilities that a
@@ -402,7 +410,10 @@ int tsfm_rope_append(void *stream, const tsfm_rope *rope, const tsfm_kv_pages *p
  *   workspace  256-byte aligned, tsfm_paged_attention_workspace() bytes; contents do not matter
  * n_heads is a multiple of n_kv_heads, M n_heads / n_kv_heads at most 65535.  Rows of tokens m >= n_new[b] are not
  * touched.  Results do not depend on the other series' lengths
- * beyond rounding, and are the same each time for the same call. */
+ * beyond rounding, and are the same each time for the same call.
+ * Made for few new tokens: every 8 to 32 (fp32: 1 to 16) of a key head's M n_heads / n_kv_heads rows read all slots that any
+ * token of the series sees, also where they belong to tokens m >= n_new[b].  A prompt of thousands of tokens is right but slow
+ * (2048 tokens, 32 heads of 128 over 8 key heads: 0.8 ms). */
 int tsfm_paged_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int64_t q_stride, void *out, int64_t out_stride,
                          const int32_t *len, const int32_t *n_new, int32_t B, int32_t M, int32_t n_heads, float scale,
                          int32_t causal, int32_t window, int32_t max_len, float *lse, const float *w_in, float *w_out,

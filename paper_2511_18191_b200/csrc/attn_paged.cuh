@@ -2,7 +2,9 @@
 //
 // Work: a unit is one series, one key head and up to ROWS of its query rows (new tokens x heads of the group: they read the
 // same keys).  A unit's slots are cut into tiles, the tiles of all units are numbered through, and every CTA takes an
-// equal run of them: lengths may differ by any factor and nothing waits for the longest series.  A run covers at most
+// equal run of them: lengths may differ by any factor and nothing waits for the longest series.  A unit's tiles are those that any of
+// the series' tokens sees, whichever rows it has: with few new tokens that is what its own rows see; with many (a prompt) most of it
+// is masked, and units whose rows lie behind n_new read it for nothing.  A run covers at most
 // two units in part, its first and its last; those leave (max, sum, unnormalised output) in the workspace, and
 // paged_join_kernel joins the parts in order.  Running maximum and sum per row, scores in base 2.
 #pragma once

@@ -3,7 +3,10 @@
 // WR x WK warps: a warp takes up to 4 query rows against 64 / WK of a tile's slots.  Eight lanes share a slot, a warp works on 8 or 16 at a
 // time, two or four a group of eight lanes, each group with its own running maximum and sum; groups, then warps, are merged when the unit ends.
 // Bound: memory up to 4 rows (64 x 8 heads of 2048 slots of 64: 88 us, 6.1 TB/s; 32 x 8 heads of 4096 slots of 128, 4 rows: 180 us, 6.0 TB/s;
-// loads straight into registers 151 and 252), instructions above (64 x 20 heads of 329 slots of 64, 9 rows: 182 us).
+// loads straight into registers 151 and 252; by cp.async, pages of 4 slots, 249 against 203 after a flush of L2).  Above: instructions and their
+// chains, not FMAs (64 x 20 heads of 329 slots of 64, 9 rows: 187 us, of which the products are some 25 at the 16 rows that they are padded to):
+// eight lanes repeat each row's maximum and exponentials, and a score takes three shuffles in a row.  Scores kept for the weights: 929 us for 32
+// series of up to 16001 slots, 4 heads of 64, 20 rows.
 #pragma once
 #include "attn_paged_fetch.cuh"
 

@@ -6,8 +6,10 @@
 // O^T = V^T P^T, P^T by one 8 x 8 transposition per eight slots): rows come in eights, not sixteens, and eight cost half of the
 // instructions and registers.  One more warp fetches (attn_paged_fetch.cuh).  Precision: scores of bf16 operands in fp32;
 // probabilities as two bf16 parts, so that only the result is rounded.
-// Bound: memory up to 16 rows (256 series of up to 8192 slots, 8 heads of 128, 4 rows: 443 us, 6.5 TB/s), the chain of a warp above
-// (32 series of up to 16001 slots, 4 heads of 64, 20 rows: 94 us, 3.6 TB/s with the scores that it writes).
+// Bound: memory where units are long and rows few (256 series of up to 8192 slots, 8 heads of 128, 4 rows: 465 us, 6.2 TB/s; one series of
+// 131071 slots: 83 us, 6.4 TB/s), the chain of a warp with 20 rows (32 series of up to 16001 slots, 4 heads of 64: 95 us, 3.5 TB/s with the
+// scores that it writes), and what starts and ends a unit where those are short (9 rows, 4.6 tiles a unit, 20 heads of 64: 32 us, 2.9 TB/s).
+// By cp.async, pages of 4 slots, 64 series of up to 8192 slots are as fast as by TMA (138 us against 142).
 #pragma once
 #include "attn_narrow.cuh"
 #include "attn_paged_fetch.cuh"

@@ -176,7 +176,7 @@ __device__ __forceinline__ void evict_select(const EvictArgs &a, EvictShared<THR
   }
 }
 
-// (a cluster only where the longest series needs more than one CTA's registers)
+// (a cluster only where the longest series' ranks take more than one CTA's shared memory)
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS, 2048 / THREADS) evict_select_kernel(EvictArgs a) {
   namespace cg = cooperative_groups;
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(THREADS, 2048 / THREADS) evict_select_kernel(E
 }
 
 // Rows of keys and values of the kept slots, 16 bytes a thread, EVICT_ROWS rows each, and their weights.  Bound: memory, where there are
-// many (32 x 8 heads of 2048 rows of 256 bytes: 83 us, 6.1 TB/s; rows one after the other, 103).
+// many (32 x 8 heads of up to 2048 rows of 256 bytes, 512 MB read and written: 83.5 us, 6.1 TB/s; rows one after the other, 103).
 template <int EVICT_ROWS>
 __global__ void __launch_bounds__(256, EVICT_ROWS == 4 ? 4 : 6) evict_copy_kernel(EvictArgs a) {
   pdl_wait();

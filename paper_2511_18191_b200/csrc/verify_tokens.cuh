@@ -36,7 +36,7 @@ struct DrawRow {
   }
   __device__ __forceinline__ double at(int t) const { return rest(p_at(t), q_at(t)); }
   // Sums over [lo, hi) by a warp, one of every `length` entries (a multiple of 256) into seg[], and all of them, in all lanes.
-  // Sixteen loads of a lane in flight: with what the compiler had gathered by itself the batch of 256 rows of 100003 took 132 us.
+  // Sixteen loads of a lane in flight (eight without q): with what the compiler had gathered by itself the batch of 256 rows of 100003 took 132 us.
   __device__ __forceinline__ double sums(int lo, int hi, int length, int lane, double *seg) const {
     return q ? sums_of<true>(lo, hi, length, lane, seg) : sums_of<false>(lo, hi, length, lane, seg);
   }
@@ -91,7 +91,8 @@ __device__ __forceinline__ int part_of(const double *part, int n, double target,
 // A cluster of CTAs a series; CTA c, and in it each warp, sums a contiguous part of the row, and keeps the sums of up to 32
 // segments of it.  The draw then falls into a CTA's, a warp's, a segment's part: 256 entries for rows of up to 32 x 256 a warp, which one
 // warp looks through; a longer segment is shared by the CTA's warps as the row was.  Sums are fp64 so that their order decides nothing.
-// Bound: memory, behind the chain proposals - their probabilities - row (256 rows of 100003, 0.8 of the proposals accepted: 43 us, 4.0 TB/s).  (In place of the segments' sums three more passes over ever
+// Bound: memory, behind the chain proposals - their probabilities - row (256 rows of 100003, 0.8 of the proposals accepted: 43 us, 4.0 TB/s; without q
+// 47 after a flush of L2: half the bytes, the same chain).  (In place of the segments' sums three more passes over ever
 // smaller parts cost 10 us.)
 __global__ void __launch_bounds__(32 * VERIFY_MAX_WARPS, 2) verify_tokens_kernel(VerifyArgs a) {
   namespace cg = cooperative_groups;
