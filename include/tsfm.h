@@ -397,8 +397,7 @@ int tsfm_rope_append(void *stream, const tsfm_rope *rope, const tsfm_kv_pages *p
  * Scores, maxima and sums are fp32 and out is rounded once.  With bf16 the probabilities enter the product with the
  * values as two bf16 parts: 2^-16 of each probability is lost, not 2^-8.  lse and w_out are fp32 throughout.
  * A token that sees nothing (or only scores of -inf) gets out 0, lse -inf.  What lies in slots that a
- * token does not see has no influence, NaN included.  A query, or a key or value in a slot that a token sees, that is not
- * finite makes the outputs that it enters not finite; whether NaN or infinite is not specified.
+ * token does not see has no influence, NaN included.  An infinite value in a slot that it sees may come out as NaN.
  *   q, out  [B, M] rows of n_heads * d_head, q_stride / out_stride elements apart
  *   lse     [B, M, n_heads] fp32, nullable
  *   w_out   nullable, [B, n_kv_heads] rows of w_stride fp32: w_out = w_in + the probabilities that a

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from tests.serving_ref import Pool
-from tests.test_gpu_serving import BF16, F32, ints, lib, stream, wide
+from tests.test_gpu_serving import BF16, F32, check_attention, ints, lib, stream, wide
 
 pytestmark = pytest.mark.gpu
 
@@ -106,3 +106,14 @@ def test_a_tile_that_does_not_arrive(dtype, D, Hq, Hkv, M, page, lengths, miss_f
         assert bad[3] == tsfm.TSFM_PAGES_TIMEOUT and lost.any() and not lost.all()
     again = attend()
     assert again[3] == 0 and all(torch.equal(x, y) for x, y in zip(again[:3], good[:3]))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("window", [0, 128, 3])
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 64), (3, 1, 128)])
+def test_prompts_beside_single_tokens(dtype, window, Hq, Hkv, D):
+    """Hundreds of new tokens, from an empty cache and behind a long one, beside series that bring one token or none: units whose rows do not exist,
+    rows that see a small part of what their unit reads."""
+    M, lengths, new = 300, [0, 500, 63, 1000, 7], [300, 1, 131, 0, 300]
+    pool = Pool(len(lengths), Hkv, D, 16, [n + m for n, m in zip(lengths, new)], dtype, seed=D)
+    check_attention(pool, dtype, Hq, Hkv, D, lengths, new, M, True, window, weights=True, qpad=8)
