@@ -117,3 +117,45 @@ def test_prompts_beside_single_tokens(dtype, window, Hq, Hkv, D):
     M, lengths, new = 300, [0, 500, 63, 1000, 7], [300, 1, 131, 0, 300]
     pool = Pool(len(lengths), Hkv, D, 16, [n + m for n, m in zip(lengths, new)], dtype, seed=D)
     check_attention(pool, dtype, Hq, Hkv, D, lengths, new, M, True, window, weights=True, qpad=8)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_captured_attention_and_eviction_on_another_stream(dtype):
+    """Both from one graph, replayed with other queries and lengths, against calls of their own; series longer than the capture saw, and shorter ones."""
+    tsfm = lib()
+    B, Hq, Hkv, D, page, longest, budget = 3, 8, 2, 64, 16, 5000, 300
+    pool = Pool(B, Hkv, D, page, [longest] * B, dtype, seed=9, spare=B * -(-budget // page))
+    dst = ints([pool.spare_ids[b::B] for b in range(B)])
+    pages, side = pool.describe(tsfm), torch.cuda.Stream()
+    size = tsfm.tsfm_paged_attention_workspace(pages, B, 1, Hq, longest, True)
+    work = torch.empty(size, dtype=torch.uint8, device="cuda")
+    q, length = torch.zeros(B, 1, Hq * D, dtype=dtype, device="cuda"), ints([1] * B)
+    names = dict(out=torch.zeros_like(q), w=torch.zeros(B, Hkv, longest, device="cuda"), w_out=torch.zeros(B, Hkv, budget, device="cuda"),
+                 kept=torch.zeros(B, Hkv, budget, dtype=torch.int32, device="cuda"), len_out=torch.zeros_like(length))
+
+    def both(s):
+        tsfm.tsfm_paged_attention(s, pages, q, Hq * D, names["out"], Hq * D, length, None, B, 1, Hq, 0.125, False, 0, longest, None, None, names["w"], longest, work, size)
+        tsfm.tsfm_cache_evict(s, pages, dst, dst.shape[1], length, names["w"], longest, B, budget, 4, 50, longest, names["kept"], names["w_out"], budget, names["len_out"])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        both(torch.cuda.current_stream().cuda_stream)
+    k0 = pool.k.clone()
+    for i, lengths in enumerate(([4000, 10, 0], [5000, 301, 300], [1, 4097, 2500])):
+        q.copy_(wide((B, 1), Hq * D, dtype, 0, 30 + i))
+        length.copy_(ints(lengths))
+        got = []
+        for replay in (True, False):
+            pool.k.copy_(k0)
+            for t in names.values():
+                t.fill_(7)
+            torch.cuda.synchronize()
+            if replay:
+                with torch.cuda.stream(side):
+                    graph.replay()
+            else:
+                both(stream())
+            torch.cuda.synchronize()
+            got.append([t.clone() for t in (*names.values(), pool.k)])
+        assert all(torch.equal(x, y) for x, y in zip(*got))
+        assert got[0][4].tolist() == [min(n, budget) for n in lengths] and int(pool.status) == 0
