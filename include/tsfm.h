@@ -471,6 +471,100 @@ int tsfm_verify_tokens(void *stream, const int32_t *tokens, const float *p, int6
                        int32_t B, int32_t K, int32_t V, const float *u, uint64_t seed, int32_t round_idx, int32_t series0,
                        const int32_t *n_draft, const int32_t *len, int32_t *out, int32_t *n_accept, int32_t *len_out);
 
+/* ---------------------------------------------------------------- trees of drafted tokens, windows with sinks, log probabilities
+ * A draft may offer several candidates for a place: M nodes of a tree in place of K proposals in a row.  Node 0 is the last
+ * committed token, which the target has not seen yet; parent[m] < m is the node that m hangs on (-1: none).  A round: tsfm_tree_init (once
+ * for a tree, whatever the number of layers; a tree that never changes is made once), per layer tsfm_rope_append_tree and
+ * tsfm_tree_attention, then tsfm_verify_tree on the target's probabilities at all nodes and tsfm_cache_commit, which
+ * moves the accepted nodes' keys and values to the front.  New tokens lie in slots len[b] + m whatever the tree.
+ * shared_tree != 0: what describes the tree (parent, mask, depth) has one row for all series in place of one a series. */
+#define TSFM_MAX_TREE 256       /* nodes of a tree */
+#define TSFM_MAX_TOP  32        /* best tokens of tsfm_token_logprobs */
+
+/* What nodes see, and how deep they are.
+ *   parent  [B, M]; one outside -1 .. m - 1 counts as -1
+ *   n_new   [B] nodes, cut to 0 .. M; NULL: M each
+ *   window  0, or as given to tsfm_tree_attention: ancestors `window` levels above or more are not seen
+ *   mask    [B, M, ceil(M / 64)] uint64 out: bit j % 64 of word j / 64 of node m: m sees j, itself or an ancestor
+ *   depth   [B, M] out: ancestors of m
+ * Nodes behind n_new get 0.  M <= TSFM_MAX_TREE. */
+int tsfm_tree_init(void *stream, const int32_t *parent, const int32_t *n_new, int32_t B, int32_t M, int32_t window, uint64_t *mask, int32_t *depth);
+
+/* tsfm_rope_append for a tree: node m has position pos[b] + depth[m] (and slot len[b] + m).  depth: [B, M] or [M]. */
+int tsfm_rope_append_tree(void *stream, const tsfm_rope *rope, const tsfm_kv_pages *pages, const void *qkv, int64_t qkv_stride, void *q_out,
+                          int64_t q_out_stride, const int32_t *pos, const int32_t *len, const int32_t *n_new, const int32_t *depth, int32_t shared_tree,
+                          int32_t B, int32_t M, int32_t n_heads);
+
+/* Attention of a tree over the cache, its nodes' keys and values already in it.  Node m < n_new[b] stands at len[b] + depth[m] and sees
+ *   slots s < len[b] with s > len[b] + depth[m] - window or s < sinks (window 0: all of them), and
+ *   slots len[b] + j, j < n_new[b], with bit j of mask[m].  (Any mask: it need not come from tsfm_tree_init.)
+ *   mask     [B, M, ceil(M / 64)] or [M, ceil(M / 64)]
+ *   depth    [B, M] or [M], cut to 0 .. M - 1; may be NULL with window 0
+ *   max_len  the longest series in slots, new ones included: lengths are cut to it.  It sizes the grid and the workspace, not the work
+ *   workspace  256-byte aligned, tsfm_tree_attention_workspace() bytes; contents do not matter
+ * Head layouts, precision, rows that see nothing, hidden slots, rows behind n_new, lse and status: as tsfm_paged_attention.
+ * M <= TSFM_MAX_TREE. */
+int tsfm_tree_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                        const int32_t *len, const int32_t *n_new, const uint64_t *mask, const int32_t *depth, int32_t shared_tree, int32_t B,
+                        int32_t M, int32_t n_heads, float scale, int32_t window, int32_t sinks, int32_t max_len, float *lse, void *workspace,
+                        size_t workspace_bytes);
+
+/* Attention of new tokens one behind the other, their keys and values already in the cache, within a sliding window that keeps the first
+ * slots visible: token m < n_new[b] sees slots s <= len[b] + m with s > len[b] + m - window or s < sinks (window 0: all of them).
+ * One token or a prompt: a token's rows read what they see.  M n_heads / n_kv_heads at most 65535.  Otherwise as
+ * tsfm_tree_attention, with its workspace. */
+int tsfm_window_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                          const int32_t *len, const int32_t *n_new, int32_t B, int32_t M, int32_t n_heads, float scale, int32_t window,
+                          int32_t sinks, int32_t max_len, float *lse, void *workspace, size_t workspace_bytes);
+
+/* Bytes of workspace for either call (host arithmetic only; of `pages` the shapes and the dtype count).  0 on invalid arguments. */
+size_t tsfm_tree_attention_workspace(const tsfm_kv_pages *pages, int32_t B, int32_t M, int32_t n_heads, int32_t max_len);
+
+/* Log probabilities of rows of logits: x = scale * logit, lse = log sum e^x, p = e^(x - lse).  A draft grows its tree from the
+ * best tokens; a server returns what was likely and how sure the model was.
+ *   logits   [rows] rows of V elements of dtype (TSFM_F32, TSFM_BF16), `stride` elements apart, at any alignment of an element
+ *   tokens   [rows, n_tokens] int32; NULL with n_tokens 0
+ *   logprob  [rows, n_tokens] out: x - lse of those tokens (outside [0, V): -inf)
+ *   lse      [rows] out, nullable;  entropy [rows] out, nullable: lse - sum p x, with p x = 0 where p is 0
+ *   top_ids  [rows, n_top] out: the n_top tokens with the largest logits, largest first, among equals the lower token first (NaN lies
+ *            below -inf); -1 behind the V-th.  top_logprob: their x - lse; -inf behind the V-th
+ * Sums are fp32.  Logits of -inf are tokens that cannot be; a row of them has lse and log probabilities -inf and entropy 0.  NaN or +inf in a
+ * row make its lse, entropy and log probabilities NaN.  scale > 0; n_top <= TSFM_MAX_TOP; V <= 2^30. */
+int tsfm_token_logprobs(void *stream, const void *logits, int64_t stride, int32_t dtype, int32_t rows, int32_t V, float scale, const int32_t *tokens,
+                        int32_t n_tokens, float *logprob, float *lse, float *entropy, int32_t n_top, int32_t *top_ids, float *top_logprob);
+
+/* Verification of a tree: from node 0 on, the children of the node reached are tried in order of their numbers; the first accepted one is
+ * reached next, and where none is, a token is drawn.  At node c, with r = p_c, Z = 1 and C = 0 at first, child j (token x) is accepted if
+ *     u_j q_c(x) Z < r(x);     else C += Z, r = max(p_c - C q_c, 0), Z = sum r
+ * in fp64: children drawn independently from q_c leave the committed tokens distributed as the target's.  q NULL: the draft's best
+ * tokens, q_c(x) is 1 at the child tried and 0 elsewhere: r loses the rejected tokens, Z their p.  The token behind the path is drawn
+ * from r as tsfm_verify_tokens draws (and from p_c where r is 0 everywhere).  Entries of p and q that are negative or not finite count as 0,
+ * uniforms are cut to [0, 1 - 2^-24], a token outside [0, V) is rejected, a node that node 0 does not lead to is not reached.
+ *   tokens, parent  [B, M] (parent: [M] with shared_tree; outside -1 .. m - 1 counts as -1); tokens[b][0] is not read as a proposal
+ *   p       [B, M] rows of V fp32, p_stride elements apart: the target's probabilities behind each node
+ *   q       [B, M] rows of V fp32, q_stride apart: the draft's; nullable
+ *   u       [B, M + 1] fp32 uniforms, one a node and the last for the draw; NULL: the Philox uniforms of tsfm_accept_round, counter
+ *           (series0 + b, round_idx, node, 0), key = seed
+ *   n_new   [B] nodes, cut to 0 .. M; NULL: M each
+ *   out     [B, M] int32: the n accepted tokens and the drawn one, -1 behind them (the drawn one is -1 too where p has no positive entry)
+ *   path    [B, M] int32: node 0 and the n accepted nodes, -1 behind them: what tsfm_cache_commit takes
+ *   n_accept [B] int32 out: n
+ *   len, len_out  [B] int32, both or neither: len_out = len + n + 1; may be the same
+ * A series without nodes commits nothing: out and path -1, n 0, len_out = len.  M <= TSFM_MAX_TREE, V <= 2^30.  Outputs overlap no input. */
+int tsfm_verify_tree(void *stream, const int32_t *tokens, const int32_t *parent, int32_t shared_tree, const float *p, int64_t p_stride, const float *q,
+                     int64_t q_stride, int32_t B, int32_t M, int32_t V, const float *u, uint64_t seed, int32_t round_idx, int32_t series0,
+                     const int32_t *n_new, const int32_t *len, int32_t *out, int32_t *path, int32_t *n_accept, int32_t *len_out);
+
+/* The accepted path's keys and values to the front: slot len[b] + path[b][i] goes to slot len[b] + i, in place, for every i up to the first
+ * entry that is negative, M or more, or not above the one before.
+ *   path      [B, M] int32, as tsfm_verify_tree writes it
+ *   len       [B] slots before the tree (not tsfm_verify_tree's len_out)
+ *   n_layers  pools that lie layer_stride elements apart, k and v alike, with one table for all (1: pages as they are)
+ * Slots outside the capacity and pages outside the pool are left alone and set bits of *status.  The pages belong to one series only.
+ * M <= TSFM_MAX_TREE. */
+int tsfm_cache_commit(void *stream, const tsfm_kv_pages *pages, const int32_t *path, const int32_t *len, int32_t B, int32_t M, int32_t n_layers,
+                      int64_t layer_stride);
+
 /* Bounds-checking mode only (TSFM_EXEC_CHECK_BOUNDS): *n_regions (nullable) receives the number of
  * guard regions of the handle.  region >= 0 additionally overwrites (damage != 0) or restores
  * (damage == 0) one byte of that guard region -- a write inside the library's own allocation --

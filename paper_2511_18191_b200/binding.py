@@ -21,6 +21,7 @@ TSFM_DRAFT_SEPARATE, TSFM_DRAFT_LAYER_SKIP = 0, 1
 TSFM_GEMM_AUTO, TSFM_GEMM_SIMT, TSFM_GEMM_WS = 0, 1, 2
 TSFM_EXEC_GRAPH, TSFM_EXEC_STREAM, TSFM_EXEC_NO_PDL, TSFM_EXEC_NO_COMPACT, TSFM_EXEC_CHECK_BOUNDS = 0, 1, 2, 4, 8
 TSFM_MAX_K = 32
+TSFM_MAX_TREE, TSFM_MAX_TOP = 256, 32
 TSFM_PAGES_BAD_ID, TSFM_PAGES_BAD_LEN, TSFM_PAGES_TIMEOUT = 1, 2, 4
 TSFM_ROPE_HALF, TSFM_ROPE_INTERLEAVED = 0, 1
 TSFM_ROPE_PLAIN, TSFM_ROPE_LINEAR, TSFM_ROPE_BASE, TSFM_ROPE_PARTS = 0, 1, 2, 3
@@ -30,6 +31,8 @@ EXPORTS = [
     "tsfm_target_only_forecast", "tsfm_draft_only_forecast", "tsfm_spec_forecast_host", "tsfm_target_only_forecast_host",
     "tsfm_spec_last_trace", "tsfm_accept_round", "tsfm_model_forward", "tsfm_gemm_bf16", "tsfm_gemm_bf16_static",
     "tsfm_rope_init", "tsfm_rope_append", "tsfm_paged_attention", "tsfm_paged_attention_workspace", "tsfm_debug_tile_wait", "tsfm_cache_evict", "tsfm_verify_tokens",
+    "tsfm_tree_init", "tsfm_rope_append_tree", "tsfm_tree_attention", "tsfm_tree_attention_workspace", "tsfm_window_attention", "tsfm_token_logprobs",
+    "tsfm_verify_tree", "tsfm_cache_commit",
     "tsfm_spec_debug_guard", "tsfm_spec_set_profiling", "tsfm_spec_kernel_profile", "tsfm_advise_block_size", "tsfm_spec_destroy", "tsfm_launch_count", "tsfm_strerror", "tsfm_last_cuda_error",
 ]
 
@@ -146,6 +149,18 @@ def _load() -> C.CDLL:
     lib.tsfm_cache_evict.argtypes = [vp, pages, vp, i32, vp, vp, i64, i32, i32, i32, i32, i32, vp, vp, i64, vp]
     lib.tsfm_verify_tokens.restype = C.c_int
     lib.tsfm_verify_tokens.argtypes = [vp, vp, vp, i64, vp, i64, i32, i32, i32, vp, u64, i32, i32, vp, vp, vp, vp, vp]
+    for name, types in (
+            ("tsfm_tree_init", [vp, vp, vp, i32, i32, i32, vp, vp]),
+            ("tsfm_rope_append_tree", [vp, C.POINTER(tsfm_rope), pages, vp, i64, vp, i64, vp, vp, vp, vp, i32, i32, i32, i32]),
+            ("tsfm_tree_attention", [vp, pages, vp, i64, vp, i64, vp, vp, vp, vp, i32, i32, i32, i32, f32, i32, i32, i32, vp, vp, sz]),
+            ("tsfm_window_attention", [vp, pages, vp, i64, vp, i64, vp, vp, i32, i32, i32, f32, i32, i32, i32, vp, vp, sz]),
+            ("tsfm_token_logprobs", [vp, vp, i64, i32, i32, i32, f32, vp, i32, vp, vp, vp, i32, vp, vp]),
+            ("tsfm_verify_tree", [vp, vp, vp, i32, vp, i64, vp, i64, i32, i32, i32, vp, u64, i32, i32, vp, vp, vp, vp, vp, vp]),
+            ("tsfm_cache_commit", [vp, pages, vp, vp, i32, i32, i32, i64])):
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = C.c_int, types
+    lib.tsfm_tree_attention_workspace.restype = sz
+    lib.tsfm_tree_attention_workspace.argtypes = [pages, i32, i32, i32, i32]
     lib.tsfm_spec_debug_guard.restype = C.c_int
     lib.tsfm_spec_debug_guard.argtypes = [vp, i32, i32, C.POINTER(i32)]
     lib.tsfm_spec_set_profiling.restype = C.c_int
@@ -336,15 +351,15 @@ def tsfm_gemm_bf16_static(stream, A, W, Cout, M: int, N: int, Kd: int) -> None:
 
 
 # ---------------------------------------------------------------- serving over a cache of pages
-_I32 = _F32 = _current_device = None            # torch's, once a tensor has come in
+_I32 = _I64 = _F32 = _current_device = None            # torch's, once a tensor has come in
 _ELEMENT: Dict[int, object] = {}
 
 
 def _torch_names() -> None:
-    global _I32, _F32, _current_device
+    global _I32, _I64, _F32, _current_device
     import torch
     _ELEMENT.update({TSFM_F32: torch.float32, TSFM_BF16: torch.bfloat16})
-    _F32, _current_device = torch.float32, torch._C._cuda_getDevice        # (asked only with a tensor of a GPU at hand)
+    _I64, _F32, _current_device = torch.int64, torch.float32, torch._C._cuda_getDevice        # (asked only with a tensor of a GPU at hand)
     _I32 = torch.int32                         # (last: it says that the others are there)
 
 
@@ -460,6 +475,86 @@ def tsfm_verify_tokens(stream, tokens, p, p_stride: int, q, q_stride: int, B: in
     _check(lib.tsfm_verify_tokens(stream, _dense(tokens, _I32, d, me), _rows(p, _F32, d, me), p_stride, _rows(q, _F32, d, me), q_stride, B, K, V,
                                   _dense(u, _F32, d, me), seed, round_idx, series0, _dense(n_draft, _I32, d, me), _dense(len, _I32, d, me),
                                   _dense(out, _I32, d, me), _dense(n_accept, _I32, d, me), _dense(len_out, _I32, d, me)), me)
+
+
+# ---------------------------------------------------------------- trees of drafted tokens, windows with sinks, log probabilities
+def _tree(t, dtype, device: int, where: str, shape) -> Optional[int]:
+    """Address of a contiguous tensor that describes a tree, of at least as many entries as `shape` has (None -> NULL)."""
+    if t is not None and t.numel() < shape:
+        raise TsfmError(TSFM_ERR_ARG, where)
+    return _dense(t, dtype, device, where)
+
+
+def tsfm_tree_init(stream, parent, n_new, B: int, M: int, window: int, mask, depth) -> None:
+    """mask: int64 (its bits are the library's uint64)."""
+    me = "tsfm_tree_init"
+    d = _device_of(parent, me)
+    _check(lib.tsfm_tree_init(stream, _tree(parent, _I32, d, me, B * M), _dense(n_new, _I32, d, me), B, M, window,
+                              _tree(mask, _I64, d, me, B * M * ((M + 63) // 64)), _tree(depth, _I32, d, me, B * M)), me)
+
+
+def tsfm_rope_append_tree(stream, rope: tsfm_rope, pages: tsfm_kv_pages, qkv, qkv_stride: int, q_out, q_out_stride: int, pos, len, n_new,
+                          depth, shared_tree: bool, B: int, M: int, n_heads: int) -> None:
+    me = "tsfm_rope_append_tree"
+    d = _device_of(len, me, pages, B)
+    e = _ELEMENT.get(pages.dtype)
+    _check(lib.tsfm_rope_append_tree(stream, rope, pages, _rows(qkv, e, d, me), qkv_stride, _rows(q_out, e, d, me), q_out_stride,
+                                     _dense(pos, _I32, d, me), _dense(len, _I32, d, me), _dense(n_new, _I32, d, me),
+                                     _tree(depth, _I32, d, me, M if shared_tree else B * M), int(bool(shared_tree)), B, M, n_heads), me)
+
+
+def tsfm_tree_attention_workspace(pages: tsfm_kv_pages, B: int, M: int, n_heads: int, max_len: int) -> int:
+    return int(lib.tsfm_tree_attention_workspace(pages, B, M, n_heads, max_len))
+
+
+def tsfm_tree_attention(stream, pages: tsfm_kv_pages, q, q_stride: int, out, out_stride: int, len, n_new, mask, depth, shared_tree: bool, B: int,
+                        M: int, n_heads: int, scale: float, window: int, sinks: int, max_len: int, lse, workspace, workspace_bytes: int) -> None:
+    me = "tsfm_tree_attention"
+    d = _device_of(len, me, pages, B)
+    e = _ELEMENT.get(pages.dtype)
+    nodes = M if shared_tree else B * M
+    _check(lib.tsfm_tree_attention(stream, pages, _rows(q, e, d, me), q_stride, _rows(out, e, d, me), out_stride, _dense(len, _I32, d, me),
+                                   _dense(n_new, _I32, d, me), _tree(mask, _I64, d, me, nodes * ((M + 63) // 64)), _tree(depth, _I32, d, me, nodes),
+                                   int(bool(shared_tree)), B, M, n_heads, scale, window, sinks, max_len, _dense(lse, _F32, d, me),
+                                   _bytes(workspace, d, me), workspace_bytes), me)
+
+
+def tsfm_window_attention(stream, pages: tsfm_kv_pages, q, q_stride: int, out, out_stride: int, len, n_new, B: int, M: int, n_heads: int, scale: float,
+                          window: int, sinks: int, max_len: int, lse, workspace, workspace_bytes: int) -> None:
+    me = "tsfm_window_attention"
+    d = _device_of(len, me, pages, B)
+    e = _ELEMENT.get(pages.dtype)
+    _check(lib.tsfm_window_attention(stream, pages, _rows(q, e, d, me), q_stride, _rows(out, e, d, me), out_stride, _dense(len, _I32, d, me),
+                                     _dense(n_new, _I32, d, me), B, M, n_heads, scale, window, sinks, max_len, _dense(lse, _F32, d, me),
+                                     _bytes(workspace, d, me), workspace_bytes), me)
+
+
+def tsfm_token_logprobs(stream, logits, stride: int, rows: int, V: int, scale: float, tokens, n_tokens: int, logprob, lse, entropy, n_top: int,
+                        top_ids, top_logprob) -> None:
+    """The library's dtype argument is that of `logits`."""
+    me = "tsfm_token_logprobs"
+    d = _device_of(logits, me)
+    code = next((c for c, e in _ELEMENT.items() if logits.dtype is e), -1) if logits.stride(-1) == 1 else -1
+    _check(lib.tsfm_token_logprobs(stream, logits.data_ptr(), stride, code, rows, V, scale, _dense(tokens, _I32, d, me), n_tokens,
+                                   _dense(logprob, _F32, d, me), _dense(lse, _F32, d, me), _dense(entropy, _F32, d, me), n_top,
+                                   _dense(top_ids, _I32, d, me), _dense(top_logprob, _F32, d, me)), me)
+
+
+def tsfm_verify_tree(stream, tokens, parent, shared_tree: bool, p, p_stride: int, q, q_stride: int, B: int, M: int, V: int, u, seed: int,
+                     round_idx: int, series0: int, n_new, len, out, path, n_accept, len_out) -> None:
+    me = "tsfm_verify_tree"
+    d = _device_of(p, me)
+    _check(lib.tsfm_verify_tree(stream, _dense(tokens, _I32, d, me), _tree(parent, _I32, d, me, M if shared_tree else B * M), int(bool(shared_tree)),
+                                _rows(p, _F32, d, me), p_stride, _rows(q, _F32, d, me), q_stride, B, M, V, _dense(u, _F32, d, me), seed, round_idx,
+                                series0, _dense(n_new, _I32, d, me), _dense(len, _I32, d, me), _dense(out, _I32, d, me), _dense(path, _I32, d, me),
+                                _dense(n_accept, _I32, d, me), _dense(len_out, _I32, d, me)), me)
+
+
+def tsfm_cache_commit(stream, pages: tsfm_kv_pages, path, len, B: int, M: int, n_layers: int = 1, layer_stride: int = 0) -> None:
+    """pages: of the first layer's pool."""
+    me = "tsfm_cache_commit"
+    d = _device_of(len, me, pages, B)
+    _check(lib.tsfm_cache_commit(stream, pages, _dense(path, _I32, d, me), _dense(len, _I32, d, me), B, M, n_layers, layer_stride), me)
 
 
 def tsfm_spec_debug_guard(h, region: int = -1, damage: bool = False) -> int:

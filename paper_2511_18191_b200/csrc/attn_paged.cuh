@@ -43,10 +43,19 @@ struct PagedAttnArgs {
   long long score_stride;
   unsigned long long wait_ns;                      // limit of a wait for a tile
   int miss_from;                                   // tests: from this tile of a CTA on more bytes are waited for than are copied
+  // of trees and windows (attn_tree.cuh) only
+  const unsigned long long *mask;                  // [B or 1][M][words], or NULL: a chain
+  const int *depth;                                // [B or 1][M], or NULL
+  long long mask_series, depth_series;             // from a series to the next: 0 with one tree for all
+  int words, sinks;
 };
 
 // The token of a query row (row / group).  Rows and groups are below 2^16, so the rounded-up reciprocal is exact.
 __device__ __forceinline__ int token_of(const PagedAttnArgs &a, int row) { return a.group == 1 ? row : (int)__umulhi((uint32_t)row, a.group_magic); }
+
+// Unit u of a series: its key head, and which of the head's row chunks it is.
+template <bool TREE> __device__ __forceinline__ int paged_unit_head(const PagedAttnArgs &a, int u) { return TREE ? u % a.pg.n_kv_heads : u / a.chunks; }
+template <bool TREE> __device__ __forceinline__ int paged_unit_chunk(const PagedAttnArgs &a, int u) { return TREE ? u / a.pg.n_kv_heads : u % a.chunks; }
 
 // A series as this call sees it: its live rows, the slots that any of them sees, the tiles that hold those.
 struct PagedSpan {
@@ -154,7 +163,8 @@ __device__ __forceinline__ T *paged_out_row(const PagedAttnArgs &a, int b, int h
 // the second of a unit's CTAs; the y blocks share its rows.  Eight warps: each a row where a unit has few parts, all of them one
 // row where it has many (one series of 131071 slots has 37: a warp alone made them a chain of loads as long as a third of the
 // kernel before).
-template <typename T, int D>
+// TREE: units are numbered as attn_tree.cuh does it.
+template <typename T, int D, bool TREE>
 __global__ void __launch_bounds__(32 * PA_JOIN_WARPS) paged_join_kernel(const __grid_constant__ PagedAttnArgs a, int ROWS) {
   constexpr int E = D / 32, W = PA_JOIN_WARPS;
   __shared__ float s_o[W][D];
@@ -163,7 +173,7 @@ __global__ void __launch_bounds__(32 * PA_JOIN_WARPS) paged_join_kernel(const __
   const PagedMeta meta = a.meta[blockIdx.x];
   if (meta.b < 0 || meta.c0 + 1 != (int)blockIdx.x) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int h = meta.u / a.chunks, row0 = (meta.u - h * a.chunks) * ROWS;
+  const int h = paged_unit_head<TREE>(a, meta.u), row0 = paged_unit_chunk<TREE>(a, meta.u) * ROWS;
   const int n_new = a.n_new ? cut(a.n_new[meta.b], a.M) : a.M;
   const int rows = min(min(ROWS, a.M * a.group - row0), n_new * a.group - row0);       // live ones
   const int parts = meta.c1 - meta.c0 + 1;

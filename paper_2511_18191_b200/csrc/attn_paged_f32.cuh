@@ -12,8 +12,9 @@
 
 namespace tsfm {
 
-template <int D_, int WROWS_, int WR_> struct PagedF32 {
+template <int D_, int WROWS_, int WR_, bool TREE_> struct PagedF32 {
   static constexpr int D = D_, WROWS = WROWS_, WR = WR_;
+  static constexpr bool TREE = TREE_;              // masks of attn_tree.cuh
   static constexpr int WARPS = D == 128 ? 8 : 4, WK = WARPS / WR, THREADS = 32 * WARPS + 32, KEYS = PA_TILE / WK;
   static constexpr int ROWS = WROWS * WR, RB = D * 4;
   static constexpr int N = WROWS == 1 && KEYS >= 16 ? 4 : 2;       // slots of a group at once
@@ -40,12 +41,14 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_f32_kernel(con
   const uint32_t smem0 = (smem_u32(paged_smem_raw) + 1023u) & ~1023u;
   unsigned char *const smem = paged_smem_raw + (smem0 - smem_u32(paged_smem_raw));
   const int R = a.M * a.group;
-  const PagedRun run = paged_find_run<C::THREADS>(a);
+  PagedRun run;
+  if constexpr (C::TREE) run = paged_find_unit_run<C::THREADS>(a, ROWS);
+  else run = paged_find_run<C::THREADS>(a);
   pdl_release();                                   // (the join waits for this grid's end; its CTAs may take their places)
   if (tid == 0) {
     PagedMeta meta{-1, 0, 0, 0};
     if (run.count > 0 && run.first) {
-      const int tiles = paged_span(a, run.b, false).tiles;
+      const int tiles = C::TREE ? paged_unit_span(a, run.b, paged_unit_chunk<true>(a, run.u), ROWS, false).tiles : paged_span(a, run.b, false).tiles;
       meta = PagedMeta{run.b, run.u, (int)(run.unit0 / run.per), (int)min((run.unit0 + tiles - 1) / run.per, (long long)gridDim.x - 1)};
     }
     a.meta[blockIdx.x] = meta;
@@ -67,14 +70,20 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_f32_kernel(con
     unsigned char *const keys = smem + stage * C::STAGE_BYTES;
     if (it.first) {
       const PagedSpan s = it.sp;
-      h = it.u / a.chunks, row0 = (it.u - h * a.chunks) * ROWS;
+      h = paged_unit_head<C::TREE>(a, it.u), row0 = paged_unit_chunk<C::TREE>(a, it.u) * ROWS;
       total = s.total, tile0 = s.tile0, tiles = s.tiles, n_new = s.n_new, seg_first = it.t;
-      min_end = paged_row_range(a, s, token_of(a, row0)).y;
-      max_start = paged_row_range(a, s, min(s.n_new, token_of(a, min(R, row0 + ROWS) - 1) + 1) - 1).x;
+      const int last = min(s.n_new, token_of(a, min(R, row0 + ROWS) - 1) + 1) - 1;
+      if constexpr (C::TREE) {
+        const int2 open = paged_tree_open(a, s, token_of(a, row0), last);
+        max_start = open.x, min_end = open.y;
+      } else {
+        min_end = paged_row_range(a, s, token_of(a, row0)).y;
+        max_start = paged_row_range(a, s, last).x;
+      }
 #pragma unroll
       for (int r = 0; r < WROWS; ++r) {
         const int own = wr * WROWS + r, row = row0 + own;
-        range[r] = row < R ? paged_row_range(a, s, token_of(a, row)) : make_int2(0, 0);
+        range[r] = row >= R ? make_int2(0, 0) : C::TREE ? paged_tree_range(a, s, it.b, token_of(a, row)) : paged_row_range(a, s, token_of(a, row));
         m[r] = -INFINITY;
         l[r] = 0.f;
 #pragma unroll
@@ -87,9 +96,20 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_f32_kernel(con
         for (int e = 0; e < E; ++e) o[r][e] = 0.f;
       }
     }
-    const int base = (tile0 + it.t) * PA_TILE;
+    const int base = C::TREE ? paged_tile_base<true>(a, it.sp, it.t) : (tile0 + it.t) * PA_TILE;
     const unsigned long long valid = sh.valid[stage][0] | (unsigned long long)sh.valid[stage][1] << 32;
     const bool open = valid == ~0ull && base >= max_start && base + PA_TILE <= min_end;      // every row sees every slot
+    unsigned long long seen[C::TREE ? WROWS : 1];  // (of a tree or a window) slots of the tile that a row sees
+    if (C::TREE && !open) {
+#pragma unroll
+      for (int r = 0; r < WROWS; ++r) {
+        const int row = row0 + wr * WROWS + r;
+        seen[C::TREE ? r : 0] = valid & paged_tree_bits(a, it.sp, range[r], it.b, row < R ? token_of(a, row) : a.M, base);
+      }
+    }
+    auto hidden = [&](int r, int at) {             // (where not every row sees every slot)
+      return C::TREE ? !(seen[C::TREE ? r : 0] >> at & 1) : base + at < range[r].x || base + at >= range[r].y || !(valid >> at & 1);
+    };
 #pragma unroll 1
     for (int k0 = wk * C::KEYS; k0 < (wk + 1) * C::KEYS; k0 += 4 * N) {
       float sc[N][WROWS];
@@ -126,7 +146,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_f32_kernel(con
 #pragma unroll
         for (int r = 0; r < WROWS; ++r) {
           sc[j][r] *= a.scale2;
-          if (!open && (slot < range[r].x || slot >= range[r].y || !(valid >> at & 1))) sc[j][r] = -INFINITY;
+          if (!open && hidden(r, at)) sc[j][r] = -INFINITY;
         }
         if (a.scores && l8 == 0 && slot < total) {
 #pragma unroll
@@ -160,14 +180,14 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_f32_kernel(con
       }
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        const int at = k0 + 4 * j + grp, slot = base + at;
+        const int at = k0 + 4 * j + grp;
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
           const float4 x = *reinterpret_cast<const float4 *>(keys + C::KV_BYTES + p * C::PART_BYTES + at * PB + tile_swz<PB>(at, l8) * 16);
 #pragma unroll
           for (int r = 0; r < WROWS; ++r) {
             // (a slot that this row does not see may hold anything: 0 x NaN must not happen)
-            if (!open && (slot < range[r].x || slot >= range[r].y || !(valid >> at & 1))) continue;
+            if (!open && hidden(r, at)) continue;
             o[r][4 * p] = fmaf(sc[j][r], x.x, o[r][4 * p]), o[r][4 * p + 1] = fmaf(sc[j][r], x.y, o[r][4 * p + 1]);
             o[r][4 * p + 2] = fmaf(sc[j][r], x.z, o[r][4 * p + 2]), o[r][4 * p + 3] = fmaf(sc[j][r], x.w, o[r][4 * p + 3]);
           }

@@ -7,7 +7,7 @@
 #pragma once
 #include <climits>
 #include "attn_flash.cuh"
-#include "attn_paged.cuh"
+#include "attn_tree.cuh"
 #include "gemm_tc.cuh"
 
 namespace tsfm {
@@ -54,7 +54,7 @@ template <int S, bool TMA> struct PagedStages {
   int dead;                                        // a tile did not arrive: what is computed from here on is NaN
 };
 
-// C: D, RB (bytes of a slot's row), PD, PB, PARTS, PART_BYTES, KV_BYTES, ROWS, STAGES, STAGE_BYTES, THREADS.
+// C: D, RB (bytes of a slot's row), PD, PB, PARTS, PART_BYTES, KV_BYTES, ROWS, STAGES, STAGE_BYTES, THREADS, TREE.
 template <typename C, bool TMA>
 __device__ __forceinline__ void paged_fetch(const PagedAttnArgs &a, const PagedRun &run, PagedStages<C::STAGES, TMA> &sh, uint32_t smem0, const CUtensorMap &mapK,
                                             const CUtensorMap &mapV) {
@@ -66,7 +66,8 @@ __device__ __forceinline__ void paged_fetch(const PagedAttnArgs &a, const PagedR
   // returned after 6000 to 17000 cycles and stood between each tile and the next.
   constexpr int AHEAD = S - 1;
   int b = run.b, u = run.u, t = run.first, ni = 0;
-  PagedSpan sp = paged_span(a, b, false);
+  int len_b = __ldg(a.len + b), new_b = a.n_new ? __ldg(a.n_new + b) : a.M;
+  PagedSpan sp = C::TREE ? paged_unit_span(a, len_b, new_b, paged_unit_chunk<true>(a, u), ROWS, false) : paged_span_of(a, len_b, new_b, false);
   int len_next = 0, new_next = 0;                // of series b + 1, looked at when it is reached
   auto fetch_next = [&]() {
     const int at = min(b + 1, a.B - 1);
@@ -92,17 +93,25 @@ __device__ __forceinline__ void paged_fetch(const PagedAttnArgs &a, const PagedR
     const int *row = a.pg.table + (long long)b * a.pg.table_stride;
 #pragma unroll
     for (int x = 0; x < (TMA ? 1 : 2); ++x) {
-      const int j = 32 * x + lane, slot = (sp.tile0 + t) * PA_TILE + (j << box_log);
-      if (j < boxes && slot + (1 << box_log) > sp.lo && slot < sp.total)
+      const int j = 32 * x + lane, slot = paged_tile_base<C::TREE>(a, sp, t) + (j << box_log);
+      if (j < boxes && paged_wants<C::TREE>(a, sp, slot, 1 << box_log))
         asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(&sh.ids[ring][j])), "l"(row + (slot >> a.pg.page_log)) : "memory");
     }
     if (lane == 0) sh.next[ring] = PagedItem{b, u, t, ni == 0 || t == 0, sp};
     if (++ni == run.count) return;
-    paged_next_tile(b, u, t, sp, a.B, a.units, [&]() {
-      const PagedSpan at = paged_span_of(a, len_next, new_next, false);
-      fetch_next();
-      return at;
-    });
+    if constexpr (C::TREE) {
+      paged_next_unit_tile(
+          a, ROWS, b, u, t, sp, len_b, new_b, [&]() {
+            len_b = len_next, new_b = new_next;
+            fetch_next();
+          });
+    } else {
+      paged_next_tile(b, u, t, sp, a.B, a.units, [&]() {
+        const PagedSpan at = paged_span_of(a, len_next, new_next, false);
+        fetch_next();
+        return at;
+      });
+    }
   };
   for (int j = 0; j < AHEAD; ++j) fetch_ids();
   flash_commit();
@@ -112,14 +121,14 @@ __device__ __forceinline__ void paged_fetch(const PagedAttnArgs &a, const PagedR
     const uint32_t dst = smem0 + stage * C::STAGE_BYTES;
     __syncwarp();
     const PagedItem it = sh.next[stage];
-    const int h = it.u / a.chunks;
-    const int base = (it.sp.tile0 + it.t) * PA_TILE;
+    const int h = paged_unit_head<C::TREE>(a, it.u);
+    const int base = paged_tile_base<C::TREE>(a, it.sp, it.t);
     long long off[2] = {-1, -1};                 // (plain copies) byte offsets of slots lane, lane + 32; -1: hidden
     int page = -1;                               // (TMA) of box lane % 8
     unsigned v[2];
     if (TMA) {
       const int j = lane & 7, slot = base + (j << box_log);
-      if (j < boxes && slot + (1 << box_log) > it.sp.lo && slot < it.sp.total) {
+      if (j < boxes && paged_wants<C::TREE>(a, it.sp, slot, 1 << box_log)) {
         page = sh.ids[stage][j];
         if ((unsigned)page >= (unsigned)a.pg.n_pages) {
           page = -1;
@@ -130,13 +139,13 @@ __device__ __forceinline__ void paged_fetch(const PagedAttnArgs &a, const PagedR
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int at = 32 * x + lane;
-        v[x] = __ballot_sync(0xffffffffu, base + at >= it.sp.lo && base + at < it.sp.total && (ok >> (at >> box_log) & 1));
+        v[x] = __ballot_sync(0xffffffffu, paged_wants<C::TREE>(a, it.sp, base + at, 1) && (ok >> (at >> box_log) & 1));
       }
     } else {
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int slot = base + 32 * x + lane;
-        if (slot >= it.sp.lo && slot < it.sp.total) {
+        if (paged_wants<C::TREE>(a, it.sp, slot, 1)) {
           const int id = sh.ids[stage][32 * x + lane];
           if ((unsigned)id < (unsigned)a.pg.n_pages) off[x] = slot_offset(a.pg, id, h, slot);
           else pages_report(a.pg, BAD_ID);
@@ -176,7 +185,7 @@ __device__ __forceinline__ void paged_fetch(const PagedAttnArgs &a, const PagedR
       }
     }
     if (it.first) {
-      const int row0 = (it.u - h * a.chunks) * ROWS;
+      const int row0 = paged_unit_chunk<C::TREE>(a, it.u) * ROWS;
 #pragma unroll 4
       for (int r = sub; r < ROWS; r += STEP) {
         const bool in = row0 + r < R;

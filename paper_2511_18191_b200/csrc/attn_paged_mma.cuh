@@ -16,8 +16,9 @@
 
 namespace tsfm {
 
-template <int D_, int NQ_, int WR_> struct PagedMma {
+template <int D_, int NQ_, int WR_, bool TREE_> struct PagedMma {
   static constexpr int D = D_, NQ = NQ_, WR = WR_;
+  static constexpr bool TREE = TREE_;              // masks of attn_tree.cuh
   static constexpr int WK = 2, KEYS = PA_TILE / WK, BLOCKS = KEYS / 16;
   static constexpr int WARPS = WR * WK, THREADS = 32 * WARPS + 32;
   static constexpr int WROWS = 8 * NQ, ROWS = WROWS * WR, RB = D * 2;
@@ -47,12 +48,14 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_mma_kernel(con
   const uint32_t smem0 = (smem_u32(paged_smem_raw) + 1023u) & ~1023u;
   unsigned char *const paged_smem = paged_smem_raw + (smem0 - smem_u32(paged_smem_raw));
   const int R = a.M * a.group;
-  const PagedRun run = paged_find_run<C::THREADS>(a);
+  PagedRun run;
+  if constexpr (C::TREE) run = paged_find_unit_run<C::THREADS>(a, ROWS);
+  else run = paged_find_run<C::THREADS>(a);
   pdl_release();                                   // (the join waits for this grid's end; its CTAs may take their places)
   if (tid == 0) {
     PagedMeta meta{-1, 0, 0, 0};
     if (run.count > 0 && run.first) {
-      const int tiles = paged_span(a, run.b, false).tiles;
+      const int tiles = C::TREE ? paged_unit_span(a, run.b, paged_unit_chunk<true>(a, run.u), ROWS, false).tiles : paged_span(a, run.b, false).tiles;
       meta = PagedMeta{run.b, run.u, (int)(run.unit0 / run.per), (int)min((run.unit0 + tiles - 1) / run.per, (long long)gridDim.x - 1)};
     }
     a.meta[blockIdx.x] = meta;
@@ -78,19 +81,25 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_mma_kernel(con
     const uint32_t kst = smem0 + stage * C::STAGE_BYTES, vst = kst + C::KV_BYTES;
     if (it.first) {
       const PagedSpan s = it.sp;
-      h = it.u / a.chunks, row0 = (it.u - h * a.chunks) * ROWS;
+      h = paged_unit_head<C::TREE>(a, it.u), row0 = paged_unit_chunk<C::TREE>(a, it.u) * ROWS;
       total = s.total, tile0 = s.tile0, tiles = s.tiles, len_lo = s.lo, n_new = s.n_new, seg_first = it.t;
 #pragma unroll
       for (int q = 0; q < NQ; ++q)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const int row = row0 + wr * WROWS + q * 8 + t4 * 2 + x;
-          range[q][x] = row < R ? paged_row_range(a, s, token_of(a, row)) : make_int2(0, 0);
+          range[q][x] = row >= R ? make_int2(0, 0) : C::TREE ? paged_tree_range(a, s, it.b, token_of(a, row)) : paged_row_range(a, s, token_of(a, row));
           m[q][x] = -INFINITY;
           l[q][x] = 0.f;
         }
-      min_end = paged_row_range(a, s, token_of(a, row0)).y;
-      max_start = paged_row_range(a, s, min(s.n_new, token_of(a, min(R, row0 + ROWS) - 1) + 1) - 1).x;
+      const int last = min(s.n_new, token_of(a, min(R, row0 + ROWS) - 1) + 1) - 1;
+      if constexpr (C::TREE) {
+        const int2 open = paged_tree_open(a, s, token_of(a, row0), last);
+        max_start = open.x, min_end = open.y;
+      } else {
+        min_end = paged_row_range(a, s, token_of(a, row0)).y;
+        max_start = paged_row_range(a, s, last).x;
+      }
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
         const int qrow = wr * WROWS + q * 8 + (lane & 7);
@@ -105,7 +114,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_mma_kernel(con
         for (int n = 0; n < D / 16; ++n) o[q][n][0] = o[q][n][1] = o[q][n][2] = o[q][n][3] = 0.f;
       }
     }
-    const int base = (tile0 + it.t) * PA_TILE, mine = base + wk * KEYS;       // slots of the tile, of this warp
+    const int base = C::TREE ? paged_tile_base<true>(a, it.sp, it.t) : (tile0 + it.t) * PA_TILE, mine = base + wk * KEYS;       // slots of the tile, of this warp
     const unsigned long long valid = sh.valid[stage][0] | (unsigned long long)sh.valid[stage][1] << 32;
 
     // scores, slots x queries
@@ -134,7 +143,24 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_mma_kernel(con
           for (int x = 0; x < 4; ++x) s[n][q][x] = (CH == 2 ? c[0][n][q][x] + c[CH - 1][n][q][x] : c[0][n][q][x]) * a.scale2;
     }
     const bool open = valid == ~0ull && base >= max_start && base + PA_TILE <= min_end;      // every row sees every slot
-    if (!open) {
+    // (of a tree or a window) bits of the warp's slots that row q, x sees
+    auto sees = [&](int q, int x) {
+      const int row = row0 + wr * WROWS + q * 8 + t4 * 2 + x;
+      return (uint32_t)(paged_tree_bits(a, it.sp, range[q][x], it.b, row < R ? token_of(a, row) : a.M, base) >> (wk * KEYS));
+    };
+    if (!open && C::TREE) {
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const uint32_t bits = sees(q, x) & (uint32_t)(valid >> (wk * KEYS));
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              if (!(bits >> (n * 16 + g + 8 * e) & 1)) s[n][q][2 * e + x] = -INFINITY;
+        }
+    } else if (!open) {
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -207,7 +233,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_mma_kernel(con
     // slots (rare) leave the products and are added to the rows that see them.
     unsigned long long odd = 0;
     const int from = max(mine, len_lo), to = min(mine + KEYS, total);
-    if (a.M > 1 && (max(from, min_end) < to || from < min(to, max_start))) {
+    if (a.M > 1 && (C::TREE ? !open : max(from, min_end) < to || from < min(to, max_start))) {
       uint32_t hit = 0;
 #pragma unroll
       for (int w = 0; w < KEYS * D / 256; ++w) {
@@ -275,7 +301,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_mma_kernel(con
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               const float p = __shfl_sync(0xffffffffu, key < 8 ? s[n][q][x] : s[n][q][2 + x], (key & 7) * 4 + t4);
-              if (slot < range[q][x].x || slot >= range[q][x].y) continue;
+              if (C::TREE ? !(sees(q, x) >> (n * 16 + key) & 1) : slot < range[q][x].x || slot >= range[q][x].y) continue;
 #pragma unroll
               for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll

@@ -1799,3 +1799,4 @@ const char *tsfm_last_cuda_error(void) { return g_cuda_err.c_str(); }
 }  // extern "C"
 
 #include "serving.cuh"
+#include "trees.cuh"

@@ -12,6 +12,8 @@ struct RopeAppendArgs {
   void *q_out;                                     // or NULL
   long long qkv_stride, q_stride;                  // elements
   const int *pos, *len, *n_new;                    // pos, n_new or NULL
+  const int *depth;                                // [B or 1][M] positions behind the first one, or NULL: m
+  long long depth_series;                          // from a series to the next
   int tokens, M, n_heads, half;                    // half: 1 pairs (i, i + rot / 2), 0 pairs (2 i, 2 i + 1)
   int pairs;                                       // rot / 2
   int parts;                                       // warps of a token
@@ -91,7 +93,7 @@ __global__ void __launch_bounds__(32 * ROPE_WARPS) rope_append_kernel(const __gr
   const int page = in ? page_of(a.pg, a.pg.table + (long long)b * a.pg.table_stride, (int)slot) : -1;
   if (page < 0 && lane == 0) pages_report(a.pg, in ? BAD_ID : BAD_LEN);
   const long long at0 = page < 0 ? 0 : slot_offset(a.pg, page, 0, (int)slot);
-  const long long t = (long long)(a.pos ? a.pos[b] : length) + m;
+  const long long t = (long long)(a.pos ? a.pos[b] : length) + (a.depth ? a.depth[b * a.depth_series + m] : m);
   for (int p = lane; p < a.pairs; p += 32) {
     const float2 c = rope_cos_sin(a.turn[p], t, a.mscale);
     cs[warp][0][p] = c.x;
@@ -150,7 +152,7 @@ __global__ void __launch_bounds__(256) rope_append_odd_kernel(const __grid_const
   __shared__ float2 cs[ROPE_MAX_PAIRS];
   const int tok = blockIdx.x, b = tok / a.M, m = tok - b * a.M;
   if (a.n_new && m >= a.n_new[b]) return;
-  if (threadIdx.x < a.pairs) cs[threadIdx.x] = rope_cos_sin(a.turn[threadIdx.x], (long long)(a.pos ? a.pos[b] : a.len[b]) + m, a.mscale);
+  if (threadIdx.x < a.pairs) cs[threadIdx.x] = rope_cos_sin(a.turn[threadIdx.x], (long long)(a.pos ? a.pos[b] : a.len[b]) + (a.depth ? a.depth[b * a.depth_series + m] : m), a.mscale);
   __syncthreads();
   const long long slot = (long long)a.len[b] + m;
   int page = -1;

@@ -91,19 +91,19 @@ struct PagedPlan {
   long long score_stride;
 };
 // The kernel of `rows` rows: f gets its configuration.
-template <int D, typename F> auto paged_variant(bf16, int rows, F f) {
-  return rows == 8 ? f(PagedMma<D, 1, 1>()) : rows == 16 ? f(PagedMma<D, 2, 1>()) : f(PagedMma<D, 2, 2>());
+template <int D, bool TREE, typename F> auto paged_variant(bf16, int rows, F f) {
+  return rows == 8 ? f(PagedMma<D, 1, 1, TREE>()) : rows == 16 ? f(PagedMma<D, 2, 1, TREE>()) : f(PagedMma<D, 2, 2, TREE>());
 }
-template <int D, typename F> auto paged_variant(float, int rows, F f) {
-  return rows == 1   ? f(PagedF32<D, 1, 1>())
-         : rows == 2 ? f(PagedF32<D, 2, 1>())
-         : rows == 4 ? f(PagedF32<D, 4, 1>())
-         : rows == 8 ? f(PagedF32<D, 4, 2>())
-                     : f(PagedF32<D, 4, 4>());
+template <int D, bool TREE, typename F> auto paged_variant(float, int rows, F f) {
+  return rows == 1   ? f(PagedF32<D, 1, 1, TREE>())
+         : rows == 2 ? f(PagedF32<D, 2, 1, TREE>())
+         : rows == 4 ? f(PagedF32<D, 4, 1, TREE>())
+         : rows == 8 ? f(PagedF32<D, 4, 2, TREE>())
+                     : f(PagedF32<D, 4, 4, TREE>());
 }
 template <typename T> int paged_ctas(int D, int rows) {
   auto ctas = [](auto c) { return decltype(c)::CTAS; };
-  return D == 32 ? paged_variant<32>(T(), rows, ctas) : D == 64 ? paged_variant<64>(T(), rows, ctas) : paged_variant<128>(T(), rows, ctas);
+  return D == 32 ? paged_variant<32, false>(T(), rows, ctas) : D == 64 ? paged_variant<64, false>(T(), rows, ctas) : paged_variant<128, false>(T(), rows, ctas);
 }
 int paged_plan(PagedPlan *pl, const tsfm_kv_pages *p, int B, int M, int n_heads, int max_len, bool weights) {
   if (int rc = pages_shape(p)) return rc;
@@ -127,6 +127,41 @@ int paged_plan(PagedPlan *pl, const tsfm_kv_pages *p, int B, int M, int n_heads,
   pl->lse2 = weights ? take(sizeof(float) * pairs * R) : 0;
   pl->scores = weights ? take(sizeof(float) * pairs * R * pl->score_stride) : 0;
   pl->bytes = at;
+  return TSFM_OK;
+}
+
+// What both attention calls say alike: the pages, the queries and outputs, the workspace.
+int paged_args(PagedAttnArgs *a, const PagedPlan &pl, const tsfm_kv_pages *pages, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+               const int32_t *len, const int32_t *n_new, int B, int M, int n_heads, float scale, int window, int max_len, float *lse,
+               void *workspace, size_t workspace_bytes) {
+  if (int rc = pages_init(&a->pg, pages)) return rc;
+  const int e = (int)elt_bytes(pages->dtype);
+  const int64_t row = (int64_t)n_heads * pages->d_head;
+  if (!aligned16(q) || !aligned16(out) || !stride_ok(q_stride, row, e) || !stride_ok(out_stride, row, e)) return TSFM_ERR_SHAPE;
+  if ((uintptr_t)workspace & 255 || workspace_bytes < pl.bytes) return TSFM_ERR_SHAPE;
+  a->pg.capacity = std::min(a->pg.capacity, max_len);
+  a->q = q;
+  a->out = out;
+  a->q_stride = q_stride;
+  a->out_stride = out_stride;
+  a->len = len;
+  a->n_new = n_new;
+  a->B = B;
+  a->M = M;
+  a->n_heads = n_heads;
+  a->group = n_heads / pages->n_kv_heads;
+  a->group_magic = (uint32_t)(((1ull << 32) + a->group - 1) / a->group);
+  a->scale2 = scale * kLog2E;
+  a->window = window;
+  a->lse = lse;
+  a->chunks = pl.chunks;
+  a->units = pages->n_kv_heads * pl.chunks;
+  char *ws = (char *)workspace;
+  a->meta = (PagedMeta *)ws;
+  a->part_ml = (float2 *)(ws + pl.part_ml);
+  a->part_o = (float *)(ws + pl.part_o);
+  a->wait_ns = g_tile_wait_ns;
+  a->miss_from = g_tile_miss_from;
   return TSFM_OK;
 }
 
@@ -159,11 +194,11 @@ cudaError_t launch_paged_tiles(cudaStream_t s, const PagedAttnArgs &a, const Pag
   return cudaGetLastError();
 }
 
-template <typename T, int D>
+template <typename T, int D, bool TREE>
 cudaError_t launch_paged(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl) {
   CUtensorMap k{}, v{};
   const bool tma = a.pg.page_log >= 3 && paged_maps(&k, &v, a.pg, D, (int)sizeof(T));
-  const cudaError_t err = paged_variant<D>(T(), pl.rows, [&](auto c) {
+  const cudaError_t err = paged_variant<D, TREE>(T(), pl.rows, [&](auto c) {
     using C = decltype(c);
     if constexpr (sizeof(T) == 2)
       return tma ? launch_paged_tiles<C>(s, a, pl, k, v, paged_attn_mma_kernel<C, true>) : launch_paged_tiles<C>(s, a, pl, k, v, paged_attn_mma_kernel<C, false>);
@@ -178,7 +213,7 @@ cudaError_t launch_paged(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan
     // (64 x 20 units of 9 rows: 8.9 us with eight blocks)
     const long long R = (long long)a.M * a.group, here = std::min<long long>(pl.rows, R);
     const unsigned rows = (unsigned)((long long)a.B * a.units * 8 >= pl.grid ? (here + PA_JOIN_WARPS - 1) / PA_JOIN_WARPS : std::min(here, 8ll));
-    if (cudaError_t e = launch_after(s, dim3(pl.grid, rows), 32 * PA_JOIN_WARPS, paged_join_kernel<T, D>, a, pl.rows)) return e;
+    if (cudaError_t e = launch_after(s, dim3(pl.grid, rows), 32 * PA_JOIN_WARPS, paged_join_kernel<T, D, TREE>, a, pl.rows)) return e;
     LAUNCHED();
   }
   if (a.w_out) {
@@ -187,6 +222,42 @@ cudaError_t launch_paged(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan
     LAUNCHED();
   }
   return cudaSuccess;
+}
+
+// depth NULL: the new tokens stand one behind the other.
+int rope_append(void *stream, const tsfm_rope *rope, const tsfm_kv_pages *pages, const void *qkv, int64_t qkv_stride, void *q_out, int64_t q_out_stride,
+                const int32_t *pos, const int32_t *len, const int32_t *n_new, const int32_t *depth, bool shared, int32_t B, int32_t M, int32_t n_heads) {
+  if (!rope || !qkv || !len || B < 1 || M < 1 || n_heads < 0 || (q_out && n_heads < 1)) return TSFM_ERR_ARG;
+  if ((rope->layout != TSFM_ROPE_HALF && rope->layout != TSFM_ROPE_INTERLEAVED) || rope->rot_dim < 0 || rope->rot_dim % 2) return TSFM_ERR_ARG;
+  RopeAppendArgs a{};
+  if (int rc = pages_init(&a.pg, pages)) return rc;
+  const int D = pages->d_head, e = (int)elt_bytes(pages->dtype);
+  const int64_t row = ((int64_t)n_heads + 2ll * pages->n_kv_heads) * D;
+  if (rope->rot_dim > D || (int64_t)B * M > kMaxGridX || row > 1 << 30) return TSFM_ERR_SHAPE;       // (elements of a row are counted in 32 bits)
+  if (!aligned16(qkv) || !stride_ok(qkv_stride, row, e)) return TSFM_ERR_SHAPE;
+  if (q_out && (!aligned16(q_out) || !stride_ok(q_out_stride, (int64_t)n_heads * D, e))) return TSFM_ERR_SHAPE;
+  if (q_out == qkv && q_out_stride != qkv_stride) return TSFM_ERR_ARG;
+  a.qkv = qkv;
+  a.q_out = q_out;
+  a.qkv_stride = qkv_stride;
+  a.q_stride = q_out_stride;
+  a.pos = pos;
+  a.len = len;
+  a.n_new = n_new;
+  a.depth = depth;
+  a.depth_series = shared ? 0 : M;
+  a.tokens = B * M;
+  a.M = M;
+  a.n_heads = n_heads;
+  a.half = rope->layout == TSFM_ROPE_HALF;
+  a.pairs = rope->rot_dim / 2;
+  a.mscale = rope->mscale;
+  std::memcpy(a.turn, rope->turn, sizeof a.turn);
+  if (pages->dtype == TSFM_BF16) launch_rope_append<bf16>((cudaStream_t)stream, a, D);
+  else launch_rope_append<float>((cudaStream_t)stream, a, D);
+  CU_TRY(cudaGetLastError());
+  LAUNCHED();
+  return TSFM_OK;
 }
 
 }  // namespace
@@ -225,35 +296,7 @@ int tsfm_rope_init(tsfm_rope *rope, int32_t layout, int32_t rot_dim, int32_t sca
 int tsfm_rope_append(void *stream, const tsfm_rope *rope, const tsfm_kv_pages *pages, const void *qkv, int64_t qkv_stride,
                      void *q_out, int64_t q_out_stride, const int32_t *pos, const int32_t *len, const int32_t *n_new,
                      int32_t B, int32_t M, int32_t n_heads) {
-  if (!rope || !qkv || !len || B < 1 || M < 1 || n_heads < 0 || (q_out && n_heads < 1)) return TSFM_ERR_ARG;
-  if ((rope->layout != TSFM_ROPE_HALF && rope->layout != TSFM_ROPE_INTERLEAVED) || rope->rot_dim < 0 || rope->rot_dim % 2) return TSFM_ERR_ARG;
-  RopeAppendArgs a{};
-  if (int rc = pages_init(&a.pg, pages)) return rc;
-  const int D = pages->d_head, e = (int)elt_bytes(pages->dtype);
-  const int64_t row = ((int64_t)n_heads + 2ll * pages->n_kv_heads) * D;
-  if (rope->rot_dim > D || (int64_t)B * M > kMaxGridX || row > 1 << 30) return TSFM_ERR_SHAPE;       // (elements of a row are counted in 32 bits)
-  if (!aligned16(qkv) || !stride_ok(qkv_stride, row, e)) return TSFM_ERR_SHAPE;
-  if (q_out && (!aligned16(q_out) || !stride_ok(q_out_stride, (int64_t)n_heads * D, e))) return TSFM_ERR_SHAPE;
-  if (q_out == qkv && q_out_stride != qkv_stride) return TSFM_ERR_ARG;
-  a.qkv = qkv;
-  a.q_out = q_out;
-  a.qkv_stride = qkv_stride;
-  a.q_stride = q_out_stride;
-  a.pos = pos;
-  a.len = len;
-  a.n_new = n_new;
-  a.tokens = B * M;
-  a.M = M;
-  a.n_heads = n_heads;
-  a.half = rope->layout == TSFM_ROPE_HALF;
-  a.pairs = rope->rot_dim / 2;
-  a.mscale = rope->mscale;
-  std::memcpy(a.turn, rope->turn, sizeof a.turn);
-  if (pages->dtype == TSFM_BF16) launch_rope_append<bf16>((cudaStream_t)stream, a, D);
-  else launch_rope_append<float>((cudaStream_t)stream, a, D);
-  CU_TRY(cudaGetLastError());
-  LAUNCHED();
-  return TSFM_OK;
+  return rope_append(stream, rope, pages, qkv, qkv_stride, q_out, q_out_stride, pos, len, n_new, nullptr, false, B, M, n_heads);
 }
 
 size_t tsfm_paged_attention_workspace(const tsfm_kv_pages *pages, int32_t B, int32_t M, int32_t n_heads, int32_t max_len,
@@ -270,48 +313,23 @@ int tsfm_paged_attention(void *stream, const tsfm_kv_pages *pages, const void *q
   PagedPlan pl;
   if (int rc = paged_plan(&pl, pages, B, M, n_heads, max_len, w_out != nullptr)) return rc;
   PagedAttnArgs a{};
-  if (int rc = pages_init(&a.pg, pages)) return rc;
-  const int D = pages->d_head, e = (int)elt_bytes(pages->dtype);
-  const int64_t row = (int64_t)n_heads * D;
-  if (!aligned16(q) || !aligned16(out) || !stride_ok(q_stride, row, e) || !stride_ok(out_stride, row, e)) return TSFM_ERR_SHAPE;
+  if (int rc = paged_args(&a, pl, pages, q, q_stride, out, out_stride, len, n_new, B, M, n_heads, scale, window, max_len, lse, workspace, workspace_bytes)) return rc;
   if (w_out && w_stride < max_len) return TSFM_ERR_SHAPE;
-  if ((uintptr_t)workspace & 255 || workspace_bytes < pl.bytes) return TSFM_ERR_SHAPE;
-  a.pg.capacity = std::min(a.pg.capacity, max_len);
-  a.q = q;
-  a.out = out;
-  a.q_stride = q_stride;
-  a.out_stride = out_stride;
-  a.len = len;
-  a.n_new = n_new;
-  a.B = B;
-  a.M = M;
-  a.n_heads = n_heads;
-  a.group = n_heads / pages->n_kv_heads;
-  a.group_magic = (uint32_t)(((1ull << 32) + a.group - 1) / a.group);
-  a.scale2 = scale * kLog2E;
+  const int D = pages->d_head;
+  char *ws = (char *)workspace;
   a.causal = causal != 0;
-  a.window = window;
-  a.lse = lse;
   a.w_in = w_in;
   a.w_out = w_out;
   a.w_stride = w_stride;
-  a.chunks = pl.chunks;
-  a.units = pages->n_kv_heads * pl.chunks;
-  char *ws = (char *)workspace;
-  a.meta = (PagedMeta *)ws;
-  a.part_ml = (float2 *)(ws + pl.part_ml);
-  a.part_o = (float *)(ws + pl.part_o);
   a.lse2 = w_out ? (float *)(ws + pl.lse2) : nullptr;
   a.scores = w_out ? (float *)(ws + pl.scores) : nullptr;
   a.score_stride = pl.score_stride;
-  a.wait_ns = g_tile_wait_ns;
-  a.miss_from = g_tile_miss_from;
   cudaStream_t s = (cudaStream_t)stream;
   cudaError_t err;
   if (pages->dtype == TSFM_BF16)
-    err = D == 32 ? launch_paged<bf16, 32>(s, a, pl) : D == 64 ? launch_paged<bf16, 64>(s, a, pl) : launch_paged<bf16, 128>(s, a, pl);
+    err = D == 32 ? launch_paged<bf16, 32, false>(s, a, pl) : D == 64 ? launch_paged<bf16, 64, false>(s, a, pl) : launch_paged<bf16, 128, false>(s, a, pl);
   else
-    err = D == 32 ? launch_paged<float, 32>(s, a, pl) : D == 64 ? launch_paged<float, 64>(s, a, pl) : launch_paged<float, 128>(s, a, pl);
+    err = D == 32 ? launch_paged<float, 32, false>(s, a, pl) : D == 64 ? launch_paged<float, 64, false>(s, a, pl) : launch_paged<float, 128, false>(s, a, pl);
   CU_TRY(err);
   return TSFM_OK;
 }
