@@ -26,7 +26,12 @@ template <bool TREE> __device__ __forceinline__ bool paged_wants(const PagedAttn
   return slot < s.total && (slot + n > s.lo || (TREE && slot < a.sinks));
 }
 
-// Span of a row chunk of a series.  lo, total: bounds of what its rows see, sinks aside.
+// Blocks of a unit.
+__device__ __forceinline__ int paged_unit_blocks(const PagedAttnArgs &a, const PagedSpan &s) {
+  return max(1, paged_sink_tiles(a, s) + max(0, (s.total + PA_TILE - 1) / PA_TILE - s.tile0));
+}
+// Span of a row chunk of a series.  lo, total: bounds of what its rows see, sinks aside.  PAIR: blocks of a tile.
+template <int PAIR = 1>
 __device__ __forceinline__ PagedSpan paged_unit_span(const PagedAttnArgs &a, int raw, int raw_new, int chunk, int rows, bool report) {
   PagedSpan s;
   s.len = cut(raw, a.pg.capacity);
@@ -39,35 +44,35 @@ __device__ __forceinline__ PagedSpan paged_unit_span(const PagedAttnArgs &a, int
   s.lo = a.window ? max(0, a.mask ? min(s.len, s.len + 1 - a.window) : s.len + m0 + 1 - a.window) : 0;
   s.tile0 = s.lo / PA_TILE;
   // (a live row without slots still has an answer: one tile)
-  s.tiles = m0 >= s.n_new ? 0 : max(1, paged_sink_tiles(a, s) + max(0, (s.total + PA_TILE - 1) / PA_TILE - s.tile0));
+  s.tiles = m0 >= s.n_new ? 0 : (paged_unit_blocks(a, s) + PAIR - 1) / PAIR;
   return s;
 }
-__device__ __forceinline__ PagedSpan paged_unit_span(const PagedAttnArgs &a, int b, int chunk, int rows, bool report) {
-  return paged_unit_span(a, __ldg(a.len + b), a.n_new ? __ldg(a.n_new + b) : a.M, chunk, rows, report);
+template <int PAIR = 1> __device__ __forceinline__ PagedSpan paged_unit_span(const PagedAttnArgs &a, int b, int chunk, int rows, bool report) {
+  return paged_unit_span<PAIR>(a, __ldg(a.len + b), a.n_new ? __ldg(a.n_new + b) : a.M, chunk, rows, report);
 }
 
 // The tile after (b, u, t) in a run; len, n_new: of series b, next() fetches those of the series behind.  Bounded by the series as
 // paged_next_tile is.
-template <typename F>
+template <int PAIR = 1, typename F>
 __device__ __forceinline__ void paged_next_unit_tile(const PagedAttnArgs &a, int rows, int &b, int &u, int &t, PagedSpan &sp, const int &len, const int &n_new, F next) {
   if (++t < sp.tiles) return;
   t = 0;
   if (++u < a.units) {
     if (u % a.pg.n_kv_heads) return;               // another head's rows of the same chunk
-    sp = paged_unit_span(a, len, n_new, u / a.pg.n_kv_heads, rows, false);
+    sp = paged_unit_span<PAIR>(a, len, n_new, u / a.pg.n_kv_heads, rows, false);
     if (sp.tiles) return;                          // (chunks behind one without live rows have none either)
   }
   u = 0;
   while (b + 1 < a.B) {
     ++b;
     next();
-    sp = paged_unit_span(a, len, n_new, 0, rows, false);
+    sp = paged_unit_span<PAIR>(a, len, n_new, 0, rows, false);
     if (sp.tiles) break;
   }
 }
 
 // As paged_find_run, over the chunks of all series: every thread sums the tiles of a contiguous share of them.
-template <int THREADS>
+template <int THREADS, int PAIR = 1>
 __device__ PagedRun paged_find_unit_run(const PagedAttnArgs &a, int rows) {
   __shared__ long long warp_sum_s[THREADS / 32];
   __shared__ PagedRun found;
@@ -79,7 +84,7 @@ __device__ PagedRun paged_find_unit_run(const PagedAttnArgs &a, int rows) {
     int len = 0, n_new = 0;
     for (long long i = i0; i < i1; ++i) {
       if (i == i0 || c == 0) len = __ldg(a.len + b), n_new = a.n_new ? __ldg(a.n_new + b) : a.M;
-      if (f(b, c, paged_unit_span(a, len, n_new, c, rows, false).tiles)) break;
+      if (f(b, c, paged_unit_span<PAIR>(a, len, n_new, c, rows, false).tiles)) break;
       if (++c == a.chunks) c = 0, ++b;
     }
   };
@@ -89,7 +94,7 @@ __device__ PagedRun paged_find_unit_run(const PagedAttnArgs &a, int rows) {
     return false;
   });
   if (blockIdx.x == 0)
-    for (int b = tid; b < a.B; b += THREADS) paged_unit_span(a, b, 0, rows, true);
+    for (int b = tid; b < a.B; b += THREADS) paged_unit_span<PAIR>(a, b, 0, rows, true);
   long long inc = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {

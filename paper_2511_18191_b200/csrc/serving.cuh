@@ -195,6 +195,19 @@ cudaError_t launch_paged_tiles(cudaStream_t s, const PagedAttnArgs &a, const Pag
 }
 
 template <typename T, int D, bool TREE>
+cudaError_t join_paged(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl) {
+  // nothing to join where no series has a second tile
+  if (a.pg.capacity <= PA_TILE || pl.grid == 1) return cudaSuccess;
+  // blocks for a unit's rows: with many units each has few parts and a block joins eight rows at once, else a block a row
+  // (64 x 20 units of 9 rows: 8.9 us with eight blocks)
+  const long long R = (long long)a.M * a.group, here = std::min<long long>(pl.rows, R);
+  const unsigned rows = (unsigned)((long long)a.B * a.units * 8 >= pl.grid ? (here + PA_JOIN_WARPS - 1) / PA_JOIN_WARPS : std::min(here, 8ll));
+  if (cudaError_t e = launch_after(s, dim3(pl.grid, rows), 32 * PA_JOIN_WARPS, paged_join_kernel<T, D, TREE>, a, pl.rows)) return e;
+  LAUNCHED();
+  return cudaSuccess;
+}
+
+template <typename T, int D, bool TREE>
 cudaError_t launch_paged(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl) {
   CUtensorMap k{}, v{};
   const bool tma = a.pg.page_log >= 3 && paged_maps(&k, &v, a.pg, D, (int)sizeof(T));
@@ -207,15 +220,7 @@ cudaError_t launch_paged(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan
   });
   if (err) return err;
   LAUNCHED();
-  // nothing to join where no series has a second tile
-  if (a.pg.capacity > PA_TILE && pl.grid > 1) {
-    // blocks for a unit's rows: with many units each has few parts and a block joins eight rows at once, else a block a row
-    // (64 x 20 units of 9 rows: 8.9 us with eight blocks)
-    const long long R = (long long)a.M * a.group, here = std::min<long long>(pl.rows, R);
-    const unsigned rows = (unsigned)((long long)a.B * a.units * 8 >= pl.grid ? (here + PA_JOIN_WARPS - 1) / PA_JOIN_WARPS : std::min(here, 8ll));
-    if (cudaError_t e = launch_after(s, dim3(pl.grid, rows), 32 * PA_JOIN_WARPS, paged_join_kernel<T, D, TREE>, a, pl.rows)) return e;
-    LAUNCHED();
-  }
+  if (cudaError_t e = join_paged<T, D, TREE>(s, a, pl)) return e;
   if (a.w_out) {
     const long long chunks = (a.pg.capacity + 511ll) / 512;
     if (cudaError_t e = launch_after(s, dim3((unsigned)(a.B * a.pg.n_kv_heads), (unsigned)std::min(chunks, 4096ll)), 128, paged_weights_kernel, a)) return e;

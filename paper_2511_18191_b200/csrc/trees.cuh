@@ -1,6 +1,7 @@
 // C entry points for trees of drafted tokens, windows with first slots, and log probabilities (the section of that name in
 // include/tsfm.h): argument checks, launch shapes.
 #pragma once
+#include "attn_tree_tc.cuh"
 #include "token_logprobs.cuh"
 #include "tree.cuh"
 #include "verify_tree.cuh"
@@ -9,14 +10,50 @@ namespace {
 
 static_assert(TREE_MAX == TSFM_MAX_TREE && LP_MAX_TOP == TSFM_MAX_TOP, "as include/tsfm.h says");
 
+#ifndef TREE_TC_MIN_ROWS
+#define TREE_TC_MIN_ROWS 33
+#endif
+// Whether the rows of a key head go to tree_attn_tc_kernel, as far as shapes say.
+bool tree_on_tc(const tsfm_kv_pages *p, int M, int n_heads) {
+  return p->dtype == TSFM_BF16 && p->d_head >= 64 && p->page_size >= 8 && (long long)M * (n_heads / p->n_kv_heads) >= TREE_TC_MIN_ROWS;
+}
+// Plan of either kernel; pl->bytes: what both would need (a pool's strides, which say whether TMA can read it, are not known here).
+int tree_plan(PagedPlan *pl, PagedPlan *tc, const tsfm_kv_pages *p, int B, int M, int n_heads, int max_len) {
+  if (int rc = paged_plan(pl, p, B, M, n_heads, max_len, false)) return rc;
+  *tc = *pl;
+  if (!tree_on_tc(p, M, n_heads)) return TSFM_OK;
+  const long long R = (long long)M * (n_heads / p->n_kv_heads), pairs = (long long)B * p->n_kv_heads;
+  tc->rows = 128;
+  tc->chunks = (int)((R + 127) / 128);
+  tc->grid = (int)std::min<long long>(pairs * tc->chunks * ((max_len + 2 * PA_TILE - 1) / (2 * PA_TILE) + 1), 2 * kSms);
+  size_t at = align256(sizeof(PagedMeta) * tc->grid);
+  tc->part_ml = at;
+  at = align256(at + sizeof(float2) * 2 * tc->grid * tc->rows);
+  tc->part_o = at;
+  tc->bytes = align256(at + sizeof(float) * 2 * tc->grid * tc->rows * p->d_head);
+  tc->bytes = pl->bytes = std::max(pl->bytes, tc->bytes);
+  return TSFM_OK;
+}
+
+template <int D> cudaError_t launch_tree_tc(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl, const CUtensorMap &k, const CUtensorMap &v) {
+  if (cudaError_t e = launch_paged_tiles<TreeTc<D>>(s, a, pl, k, v, tree_attn_tc_kernel<TreeTc<D>>)) return e;
+  LAUNCHED();
+  return join_paged<bf16, D, true>(s, a, pl);
+}
+
 // tsfm_tree_attention (mask or a chain) and tsfm_window_attention
 int tree_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int64_t q_stride, void *out, int64_t out_stride, const int32_t *len,
                    const int32_t *n_new, const uint64_t *mask, const int32_t *depth, bool shared, int32_t B, int32_t M, int32_t n_heads, float scale,
                    int32_t window, int32_t sinks, int32_t max_len, float *lse, void *workspace, size_t workspace_bytes) {
   if (!q || !out || !len || !workspace || window < 0 || sinks < 0 || !std::isfinite(scale * kLog2E)) return TSFM_ERR_ARG;
-  PagedPlan pl;
-  if (int rc = paged_plan(&pl, pages, B, M, n_heads, max_len, false)) return rc;
+  PagedPlan pl, tc;
+  if (int rc = tree_plan(&pl, &tc, pages, B, M, n_heads, max_len)) return rc;
   PagedAttnArgs a{};
+  CUtensorMap k{}, v{};
+  if (tree_on_tc(pages, M, n_heads)) {
+    if (int rc = pages_init(&a.pg, pages)) return rc;
+    if (paged_maps(&k, &v, a.pg, pages->d_head, 2)) pl = tc;
+  }
   if (int rc = paged_args(&a, pl, pages, q, q_stride, out, out_stride, len, n_new, B, M, n_heads, scale, window, max_len, lse, workspace, workspace_bytes)) return rc;
   a.causal = 1;
   a.mask = (const unsigned long long *)mask;
@@ -28,7 +65,9 @@ int tree_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int6
   cudaStream_t s = (cudaStream_t)stream;
   const int D = pages->d_head;
   cudaError_t err;
-  if (pages->dtype == TSFM_BF16)
+  if (pl.rows == 128)
+    err = D == 64 ? launch_tree_tc<64>(s, a, pl, k, v) : launch_tree_tc<128>(s, a, pl, k, v);
+  else if (pages->dtype == TSFM_BF16)
     err = D == 32 ? launch_paged<bf16, 32, true>(s, a, pl) : D == 64 ? launch_paged<bf16, 64, true>(s, a, pl) : launch_paged<bf16, 128, true>(s, a, pl);
   else
     err = D == 32 ? launch_paged<float, 32, true>(s, a, pl) : D == 64 ? launch_paged<float, 64, true>(s, a, pl) : launch_paged<float, 128, true>(s, a, pl);
@@ -57,8 +96,8 @@ int tsfm_rope_append_tree(void *stream, const tsfm_rope *rope, const tsfm_kv_pag
 }
 
 size_t tsfm_tree_attention_workspace(const tsfm_kv_pages *pages, int32_t B, int32_t M, int32_t n_heads, int32_t max_len) {
-  PagedPlan pl;
-  return paged_plan(&pl, pages, B, M, n_heads, max_len, false) ? 0 : pl.bytes;
+  PagedPlan pl, tc;
+  return tree_plan(&pl, &tc, pages, B, M, n_heads, max_len) ? 0 : pl.bytes;
 }
 
 int tsfm_tree_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int64_t q_stride, void *out, int64_t out_stride,
