@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_f32_kernel(con
   unsigned char *const smem = paged_smem_raw + (smem0 - smem_u32(paged_smem_raw));
   const int R = a.M * a.group;
   PagedRun run;
-  if constexpr (C::TREE) run = paged_find_unit_run<C::THREADS>(a, ROWS);
+  if constexpr (C::TREE) run = paged_find_unit_run<C::THREADS>(a, ROWS, 1);
   else run = paged_find_run<C::THREADS>(a);
   pdl_release();                                   // (the join waits for this grid's end; its CTAs may take their places)
   if (tid == 0) {

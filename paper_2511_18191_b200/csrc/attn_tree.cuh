@@ -71,59 +71,71 @@ __device__ __forceinline__ void paged_next_unit_tile(const PagedAttnArgs &a, int
   }
 }
 
-// As paged_find_run, over the chunks of all series: every thread sums the tiles of a contiguous share of them.
+// As paged_find_run, over the chunks of all series: every thread sums up a contiguous share of them.  What starts and ends a unit counts as
+// `start` tiles, in front of its own, so that runs of many short units are as long as those of few long ones.  (unit0: place of the unit's first
+// tile on this scale.)
 template <int THREADS, int PAIR = 1>
-__device__ PagedRun paged_find_unit_run(const PagedAttnArgs &a, int rows) {
-  __shared__ long long warp_sum_s[THREADS / 32];
+__device__ PagedRun paged_find_unit_run(const PagedAttnArgs &a, int rows, int start) {
+  __shared__ long long warp_sum_s[2][THREADS / 32];
   __shared__ PagedRun found;
+  __shared__ long long tiles_to[2];                // tiles before the run, before its end
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, Hkv = a.pg.n_kv_heads;
   const long long items = (long long)a.B * a.chunks, share = (items + THREADS - 1) / THREADS;
   const long long i0 = min(items, tid * share), i1 = min(items, i0 + share);
-  auto each = [&](auto f) {                        // f(series, chunk, tiles of one head) until it says so
+  auto each = [&](auto f) {                        // f(series, chunk, tiles of one head)
     int b = (int)(i0 / a.chunks), c = (int)(i0 - (long long)b * a.chunks);
     int len = 0, n_new = 0;
     for (long long i = i0; i < i1; ++i) {
       if (i == i0 || c == 0) len = __ldg(a.len + b), n_new = a.n_new ? __ldg(a.n_new + b) : a.M;
-      if (f(b, c, paged_unit_span<PAIR>(a, len, n_new, c, rows, false).tiles)) break;
+      f(b, c, paged_unit_span<PAIR>(a, len, n_new, c, rows, false).tiles);
       if (++c == a.chunks) c = 0, ++b;
     }
   };
-  long long mine = 0;
+  long long mine = 0, own_tiles = 0;
   each([&](int b, int c, int tiles) {
-    mine += (long long)tiles * Hkv;
-    return false;
+    own_tiles += (long long)tiles * Hkv;
+    mine += tiles ? (long long)(tiles + start) * Hkv : 0;
   });
   if (blockIdx.x == 0)
     for (int b = tid; b < a.B; b += THREADS) paged_unit_span<PAIR>(a, b, 0, rows, true);
-  long long inc = mine;
+  long long inc = mine, tiles_inc = own_tiles;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += v;
+    const long long v = __shfl_up_sync(0xffffffffu, inc, o), w = __shfl_up_sync(0xffffffffu, tiles_inc, o);
+    if (lane >= o) inc += v, tiles_inc += w;
   }
-  if (lane == 31) warp_sum_s[warp] = inc;
-  if (tid == 0) found.b = -1, found.count = 0;
+  if (lane == 31) warp_sum_s[0][warp] = inc, warp_sum_s[1][warp] = tiles_inc;
+  if (tid == 0) found.b = -1;
   __syncthreads();
-  long long before = inc - mine, total = 0;
+  long long before = inc - mine, tiles_before = tiles_inc - own_tiles, total = 0, all_tiles = 0;
   for (int i = 0; i < THREADS / 32; ++i) {
-    if (i < warp) before += warp_sum_s[i];
-    total += warp_sum_s[i];
+    if (i < warp) before += warp_sum_s[0][i], tiles_before += warp_sum_s[1][i];
+    total += warp_sum_s[0][i];
+    all_tiles += warp_sum_s[1][i];
   }
-  const long long per = max(1ll, (total + gridDim.x - 1) / gridDim.x), start = per * blockIdx.x;
-  if (start >= before && start < before + mine) {
+  const long long per = max(1ll, (total + gridDim.x - 1) / gridDim.x), begin = per * blockIdx.x, end = begin + per;
+  if (tid == 0) {
+    if (begin >= total) tiles_to[0] = all_tiles;
+    if (end >= total) tiles_to[1] = all_tiles;
+  }
+  if ((begin >= before && begin < before + mine) || (end >= before && end < before + mine)) {
     each([&](int b, int c, int tiles) {
-      const long long here = (long long)tiles * Hkv;
-      if (start >= before + here) {
-        before += here;
-        return false;
+      const long long unit = tiles ? tiles + start : 0, here = unit * Hkv;
+      for (int x = 0; x < 2; ++x) {
+        const long long at = x ? end : begin;
+        if (at < before || at >= before + here) continue;
+        const int h = (int)((at - before) / unit), first = (int)((at - before) - h * unit);
+        tiles_to[x] = tiles_before + (long long)h * tiles + max(0, first - start);
+        if (!x) found = PagedRun{b, c * Hkv + h, max(0, first - start), 0, before + h * unit + start, per};
       }
-      const int h = (int)((start - before) / tiles), first = (int)((start - before) - (long long)h * tiles);
-      found = PagedRun{b, c * Hkv + h, first, (int)min(per, total - start), start - first, per};
-      return true;
+      before += here;
+      tiles_before += (long long)tiles * Hkv;
     });
   }
   __syncthreads();
-  return found;
+  PagedRun run = found;
+  run.count = (int)(tiles_to[1] - tiles_to[0]);
+  return run;
 }
 
 // Slots [x, y) are the window of token m, in a tree below len.

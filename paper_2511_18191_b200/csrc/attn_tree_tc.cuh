@@ -1,47 +1,63 @@
 // Attention of many rows over a cache of pages (trees of some dozens of nodes, prompts; masks of attn_tree.cuh) on the tensor cores:
 // tcgen05, bf16, heads of 64 and 128, pages of eight slots and more.
 //
-// A CTA takes a run of tiles as in attn_paged.cuh, of units of 128 rows (new tokens x the heads of a group).  A tile is two blocks of 64 slots,
-// wherever in the cache they lie (a block with sinks beside one of the window).  Of each:
+// A CTA takes a run of tiles as in attn_paged.cuh, of units of QT x 128 rows (new tokens x the heads of a group).  A tile is two blocks of 64 slots,
+// wherever in the cache they lie (a block with sinks beside one of the window).  Of each, for 128 rows at a time:
 //   S = Q K^T (128 x 128, queries and keys as they are: products of bf16, sums in fp32, in tensor memory); softmax by two threads a row, each
-//   the slots of one block: maximum, exponentials, sum; P back over S as bf16; O += P V in tensor memory.
-// The exponentials' reference moves only when a row's maximum passes it by 2^8 (and then O is multiplied in tensor memory): softmax is the same for
-// every reference, and 2^8 times the largest sum is far from where fp32 ends.  So O is read once, when the unit ends.
-// Two CTAs on an SM: one's products run beside the other's softmax.
+//   the slots of one block: exponentials, sum, maximum; P back over S as bf16; O += P V in tensor memory.
+// Softmax is the same whatever is subtracted from the scores, as long as nothing overflows and the largest terms do not vanish.  So the exponentials
+// do not wait for the row's maximum: they are taken against a reference, 0 at first, and where the maximum turns out to lie 2^20 above it (the first
+// one: or below) the reference moves there, O is multiplied in tensor memory and the tile's exponentials are taken again.  With scores of ordinary size
+// that never happens, and O is read once, when the unit ends.  (Values above 2^100 could so overflow where a sum over 1 would not.)
+// QT = 1: two CTAs on an SM, one's products run beside the other's softmax.  QT = 2: one CTA with two times 128 rows, which share the tiles that
+// they read and take turns in the same way.
 // A slot that some row must not see never meets it as 0 x NaN: values outside the series' slots are zeroed in shared memory; in tiles that not every
 // row sees as a whole, values that are not finite are zeroed too, and rows that do see one get NaN.
-// Warps 0-7 softmax (row 32 (w % 4) + lane, block w / 4), 8 fetches (TMA boxes of a page, queries by cp.async), 9 tensor memory and products.  Every
-// wait is bounded; when one runs out the status says so and what depends on it is NaN.
+// Warps 0 .. 8 QT - 1 softmax (row 32 (w % 4) + lane of 128, block w / 4 % 2), then one that fetches (TMA: boxes of a page, queries) and one for tensor
+// memory and products.  Every wait is bounded; when one runs out the status says so and what depends on it is NaN.
 #pragma once
 #include "attn_mma.cuh"
 #include "attn_paged_fetch.cuh"
 
 namespace tsfm {
 
-template <int D_> struct TreeTc {
-  static constexpr int D = D_, ROWS = 128, RB = D * 2, PARTS = D / 64;
+template <int D_, int QT_> struct TreeTc {
+  static constexpr int D = D_, QT = QT_, ROWS = 128 * QT, RB = D * 2, PARTS = D / 64;
   static constexpr int PART_BYTES = 128 * 128;                   // 128 rows (slots, queries) of 64 elements
   static constexpr int TILE_BYTES = PARTS * PART_BYTES;
-  static constexpr int STAGES = D == 128 ? 1 : 2;                // of keys and of values
-  static constexpr int SMEM_BYTES = (1 + 2 * STAGES) * TILE_BYTES + 1024;        // (queries first; parts begin at multiples of 1 KB)
-  static constexpr int WARPS = 8, THREADS = 32 * (WARPS + 2), CTAS = 2;
-  static constexpr int COLS = 256, S = 0, O = 128;               // columns of tensor memory; a block's probabilities lie over its scores
-  static_assert(CTAS * (SMEM_BYTES + 4096) <= 227 * 1024, "two CTAs on an SM");
+  static constexpr int STAGES = D == 128 && QT == 1 ? 1 : 2;     // of keys and of values
+  static constexpr int SMEM_BYTES = (QT + 2 * STAGES) * TILE_BYTES + 1024;       // (queries first; parts begin at multiples of 1 KB)
+  static constexpr int WARPS = 8 * QT, THREADS = 32 * (WARPS + 2), CTAS = 2 / QT;
+  static constexpr int COLS = 256 * QT, O = 128 * QT;            // columns of tensor memory: scores, sums; a block's probabilities lie over its scores
+  static constexpr int START = 2;                                // what starts and ends a unit, in tiles
+  static_assert(CTAS * (SMEM_BYTES + 5 * 1024) <= 228 * 1024, "CTAs on an SM");
 };
-constexpr float TREE_TC_SLACK = 8.f;               // a row's maximum may pass the reference by so many powers of two
+constexpr float TREE_TC_SLACK = 20.f;              // powers of two between a row's maximum and its reference
 
 struct TreeTcShared {
-  unsigned long long kfull[2], kempty[2], vfull[2], vempty[2], info[4], q_ready, s_full, p_ready, o_full, looked, drained;
+  unsigned long long kfull[2], kempty[2], vfull[2], vempty[2], info[4], s_full[2], p_ready[2], o_full[2], looked[2], q_ready, drained;
   unsigned long long valid[4][2];                  // of a tile's blocks: slots that exist
-  float top[2][128], sum[2][128];                  // what the two threads of a row exchange
-  uint32_t bad[2][4];                              // slots of the tile whose values are not finite; of the next such tile: none yet
+  float top[2][2][128], sum[2][2][128];            // what the two threads of a row exchange
+  uint32_t bad[4][4];                              // slots of such a tile whose values are not finite
   uint32_t tmem;
 };
 
 // A CTA's way through its run; every role walks by itself.
 struct TreeWalk {
   int b, u, t, len, n_new, len_next, new_next;
+  int blocks, sink, gap;                           // of the unit: its blocks, those with sinks, slots between these and the others
   PagedSpan sp;
+  __device__ __forceinline__ void unit(const PagedAttnArgs &a) {
+    blocks = paged_unit_blocks(a, sp);
+    sink = paged_sink_tiles(a, sp);
+    gap = (sp.tile0 - sink) * PA_TILE;
+  }
+  // First slot of block x of the tile; whether it is one.
+  __device__ __forceinline__ int base(int x) const {
+    const int k = 2 * t + x;
+    return k * PA_TILE + (k < sink ? 0 : gap);
+  }
+  __device__ __forceinline__ bool two() const { return 2 * t + 1 < blocks; }
   __device__ __forceinline__ void peek(const PagedAttnArgs &a) {
     const int at = min(b + 1, a.B - 1);
     len_next = __ldg(a.len + at);
@@ -51,6 +67,7 @@ struct TreeWalk {
     len = __ldg(a.len + b);
     n_new = a.n_new ? __ldg(a.n_new + b) : a.M;
     sp = paged_unit_span<2>(a, len, n_new, u / a.pg.n_kv_heads, rows, false);
+    unit(a);
     peek(a);
   }
   __device__ __forceinline__ void next(const PagedAttnArgs &a, int rows) {
@@ -58,35 +75,61 @@ struct TreeWalk {
       len = len_next, n_new = new_next;
       peek(a);
     });
+    if (t == 0) unit(a);
+  }
+  // How many times 128 rows of the unit hold a live one.
+  template <int QT> __device__ __forceinline__ int halves(const PagedAttnArgs &a) const {
+    return QT == 2 && sp.n_new * (long long)a.group - u / a.pg.n_kv_heads * (128ll * QT) > 128 ? 2 : 1;
   }
 };
 
-__device__ __forceinline__ void tmem_load32(uint32_t taddr, float *v) {        // (the caller waits)
+__device__ __forceinline__ void tmem_load16(uint32_t taddr, float (&v)[16]) {        // (tmem_wait16 behind it)
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
-      "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
       : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
-        "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]),
-        "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]),
-        "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+        "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
       : "r"(taddr) : "memory");
 }
+// (names the values: nothing that uses them moves in front of the wait)
+__device__ __forceinline__ void tmem_wait16(float (&v)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]),
+                 "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15])
+               :: "memory");
+}
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tma_load_queries(uint32_t dst, const CUtensorMap *map, int x, int head, int token, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(map), "r"(x), "r"(head), "r"(token), "r"(bar) : "memory");
+}
+// Barrier of 64 threads that says whether any of them brought true.
+__device__ __forceinline__ bool bar_any64(int id, bool mine) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(any) : "r"((uint32_t)mine), "r"(id) : "memory");
+  return any != 0;
+}
 
+// q_tma: mapQ is there (a group divides 128); else queries come by cp.async, a row at a time.
 template <typename C>
-__global__ void __launch_bounds__(C::THREADS, C::CTAS) tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV) {
-  constexpr int D = C::D, ROWS = C::ROWS, ST = C::STAGES, PARTS = C::PARTS;
+__global__ void __launch_bounds__(C::THREADS, C::CTAS)
+tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
+                    const __grid_constant__ CUtensorMap mapQ, int q_tma) {
+  constexpr int D = C::D, ROWS = C::ROWS, ST = C::STAGES, PARTS = C::PARTS, QT = C::QT;
   extern __shared__ __align__(1024) unsigned char paged_smem_raw[];
   __shared__ TreeTcShared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), Hkv = a.pg.n_kv_heads;
   const uint32_t smem0 = (smem_u32(paged_smem_raw) + 1023u) & ~1023u;
   unsigned char *const smem = paged_smem_raw + (smem0 - smem_u32(paged_smem_raw));
-  const uint32_t keys0 = smem0 + C::TILE_BYTES, values0 = keys0 + ST * C::TILE_BYTES;
+  const uint32_t keys0 = smem0 + QT * C::TILE_BYTES, values0 = keys0 + ST * C::TILE_BYTES;
   const uint32_t kfull = smem_u32(sh.kfull), kempty = smem_u32(sh.kempty), vfull = smem_u32(sh.vfull), vempty = smem_u32(sh.vempty), info = smem_u32(sh.info);
-  const uint32_t q_ready = smem_u32(&sh.q_ready), s_full = smem_u32(&sh.s_full), p_ready = smem_u32(&sh.p_ready), o_full = smem_u32(&sh.o_full),
-                 looked = smem_u32(&sh.looked), drained = smem_u32(&sh.drained);
+  const uint32_t q_ready = smem_u32(&sh.q_ready), s_full = smem_u32(sh.s_full), p_ready = smem_u32(sh.p_ready), o_full = smem_u32(sh.o_full),
+                 looked = smem_u32(sh.looked), drained = smem_u32(&sh.drained);
   const int R = a.M * a.group;
-  const PagedRun run = paged_find_unit_run<C::THREADS, 2>(a, ROWS);
+  const PagedRun run = paged_find_unit_run<C::THREADS, 2>(a, ROWS, C::START);
   pdl_release();                                   // (the join waits for this grid's end; its CTAs may take their places)
   if (tid == 0) {
     PagedMeta meta{-1, 0, 0, 0};
@@ -99,20 +142,20 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) tree_attn_tc_kernel(const
   if (run.count == 0) return;
   const bool leader = elect_one();
   if (warp == C::WARPS) {
-    if (lane < ST) {
+    if (lane < 2) {
       mbar_init(kfull + 8 * lane, 1);
       mbar_init(kempty + 8 * lane, 1);
       mbar_init(vfull + 8 * lane, 1);
       mbar_init(vempty + 8 * lane, 1);
+      mbar_init(s_full + 8 * lane, 1);
+      mbar_init(p_ready + 8 * lane, 8);
+      mbar_init(o_full + 8 * lane, 1);
+      mbar_init(looked + 8 * lane, 8);
     }
     if (lane < 4) mbar_init(info + 8 * lane, 1);
-    if (lane < 8) (&sh.bad[0][0])[lane] = 0;
+    if (lane < 16) (&sh.bad[0][0])[lane] = 0;
     if (lane == 0) {
       mbar_init(q_ready, 1);
-      mbar_init(s_full, 1);
-      mbar_init(p_ready, C::WARPS);
-      mbar_init(o_full, 1);
-      mbar_init(looked, C::WARPS);
       mbar_init(drained, 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -138,55 +181,37 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) tree_attn_tc_kernel(const
     // ---------------- fetches
     const int box_log = min(a.pg.page_log, 6), boxes = PA_TILE >> box_log;
     TreeWalk ahead(a, run, ROWS);                  // the tile whose page ids are looked up; lane 8 h + j: box j of block h
+    int id = 0;                                    // (not looked at before its tile's turn: nothing waits for the load until then)
+    bool asked = false;
+    int h = 0;
     auto look_up = [&]() {
       const int h = lane >> 3, j = lane & 7;
-      if (h > 1 || j >= boxes || 2 * ahead.t + h >= paged_unit_blocks(a, ahead.sp)) return -1;
-      const int slot = paged_tile_base<true>(a, ahead.sp, 2 * ahead.t + h) + (j << box_log);
-      if (!paged_wants<true>(a, ahead.sp, slot, 1 << box_log)) return -1;
-      const int id = __ldg(a.pg.table + (long long)ahead.b * a.pg.table_stride + (slot >> a.pg.page_log));
-      return (unsigned)id < (unsigned)a.pg.n_pages ? id : -2;
+      asked = h < 2 && j < boxes && (h == 0 || ahead.two());
+      const int slot = ahead.base(h) + (j << box_log);
+      asked = asked && paged_wants<true>(a, ahead.sp, slot, 1 << box_log);
+      if (asked) id = __ldg(a.pg.table + (long long)ahead.b * a.pg.table_stride + (slot >> a.pg.page_log));
     };
-    int id = look_up();
+    look_up();
     for (int i = 0; i < run.count && ok; ++i) {
-      const int stage = i % ST, use = i / ST, page = id;
+      const int stage = i % ST, use = i / ST, page = asked && (unsigned)id < (unsigned)a.pg.n_pages ? id : -1;
+      if (__any_sync(0xffffffffu, asked && page < 0)) pages_report(a.pg, BAD_ID);
       const TreeWalk at = ahead;
       if (i + 1 < run.count) {
         ahead.next(a, ROWS);
-        id = look_up();
+        look_up();
       }
       const bool first = i == 0 || at.t == 0;
-      if (__any_sync(0xffffffffu, page == -2)) pages_report(a.pg, BAD_ID);
       const unsigned got = __ballot_sync(0xffffffffu, page >= 0);
-      if (i >= ST) wait(kempty + 8 * stage, use - 1);
-      if (first && i) wait(kempty + 8 * ((i - 1) % ST), (i - 1) / ST);        // the queries' last products are done
-      const int h = at.u % Hkv, blocks = paged_unit_blocks(a, at.sp);
+      if (first) h = at.u % Hkv;
+      const bool two = at.two();
       int base[2];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) base[x] = paged_tile_base<true>(a, at.sp, 2 * at.t + x);
+      for (int x = 0; x < 2; ++x) base[x] = at.base(x);
       unsigned v[4];
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const int s = (x & 1) * 32 + lane;
-        v[x] = __ballot_sync(0xffffffffu, 2 * at.t + (x >> 1) < blocks && paged_wants<true>(a, at.sp, base[x >> 1] + s, 1) && (got >> ((x >> 1) * 8 + (s >> box_log)) & 1));
-      }
-      if (!ok) break;
-      if (first) {
-        const int row0 = at.u / Hkv * ROWS;
-        constexpr int CPR = C::RB / 16;            // 16-byte chunks of a row
-#pragma unroll 4
-        for (int e = lane; e < ROWS * CPR; e += 32) {
-          const int r = e / CPR, chunk = e % CPR;
-          const bool in = row0 + r < R;
-          const int tok = in ? token_of(a, row0 + r) : 0, head = h * a.group + (in ? row0 + r - tok * a.group : 0);
-          const char *src = reinterpret_cast<const char *>(a.q) + (((long long)at.b * a.M + tok) * a.q_stride + (long long)head * D) * 2 + chunk * 16;
-          const uint32_t dst = smem0 + chunk / 8 * C::PART_BYTES + r * 128 + ((chunk & 7) ^ (r & 7)) * 16;
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
-        }
-      }
-      if (lane == 0) {
-        sh.valid[i & 3][0] = v[0] | (unsigned long long)v[1] << 32;
-        sh.valid[i & 3][1] = v[2] | (unsigned long long)v[3] << 32;
-        mbar_arrive(info + 8 * (i & 3));
+        v[x] = __ballot_sync(0xffffffffu, (x < 2 || two) && paged_wants<true>(a, at.sp, base[x >> 1] + s, 1) && (got >> ((x >> 1) * 8 + (s >> box_log)) & 1));
       }
       auto issue = [&](uint32_t dst, const CUtensorMap *map, uint32_t bar, int more) {
         if (lane == 0) mbar_expect_tx(bar, __popc(got) * (PARTS * 128 << box_log) + more);
@@ -199,12 +224,41 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) tree_attn_tc_kernel(const
         }
         __syncwarp();
       };
+      if (i >= ST) wait(kempty + 8 * stage, use - 1);
+      if (!ok) break;
+      if (lane == 0) {
+        sh.valid[i & 3][0] = v[0] | (unsigned long long)v[1] << 32;
+        sh.valid[i & 3][1] = v[2] | (unsigned long long)v[3] << 32;
+        mbar_arrive(info + 8 * (i & 3));
+      }
       issue(keys0 + stage * C::TILE_BYTES, &mapK, kfull + 8 * stage, i >= a.miss_from ? 16 : 0);
       if (first) {
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(q_ready);
+        if (i) wait(kempty + 8 * ((i - 1) % ST), (i - 1) / ST);          // the queries' last products are done
+        if (!ok) break;
+        const int row0 = at.u / Hkv * ROWS, halves = at.halves<QT>(a);
+        if (q_tma) {
+          if (lane == 0) mbar_expect_tx(q_ready, halves * C::TILE_BYTES);
+          __syncwarp();
+          if (lane < halves * PARTS) {
+            const int q = lane / PARTS, p = lane % PARTS;
+            tma_load_queries(smem0 + q * C::TILE_BYTES + p * C::PART_BYTES, &mapQ, p * 64, h * a.group, at.b * a.M + token_of(a, row0 + q * 128), q_ready);
+          }
+        } else {
+          constexpr int CPR = C::RB / 16;          // 16-byte chunks of a row
+#pragma unroll 4
+          for (int e = lane; e < halves * 128 * CPR; e += 32) {
+            const int r = e / CPR, chunk = e % CPR;
+            const bool in = row0 + r < R;
+            const int tok = in ? token_of(a, row0 + r) : 0, head = h * a.group + (in ? row0 + r - tok * a.group : 0);
+            const char *src = reinterpret_cast<const char *>(a.q) + (((long long)at.b * a.M + tok) * a.q_stride + (long long)head * D) * 2 + chunk * 16;
+            const uint32_t dst = smem0 + r / 128 * C::TILE_BYTES + chunk / 8 * C::PART_BYTES + r % 128 * 128 + ((chunk & 7) ^ (r & 7)) * 16;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+          }
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(q_ready);
+        }
       }
       if (i >= ST) wait(vempty + 8 * stage, use - 1);
       if (!ok) break;
@@ -214,47 +268,63 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) tree_attn_tc_kernel(const
     // ---------------- products (the warp as a whole, one lane issues)
     constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);
     constexpr uint32_t idesc_o = idesc | (1u << 16) | ((64u >> 3) << 17);
-    const uint64_t dq = umma_smem_desc(smem0);
     TreeWalk at(a, run, ROWS);
-    int units = 0;
-    for (int i = 0; i < run.count; ++i) {
-      const int stage = i % ST, use = i / ST;
-      const bool first = i == 0 || at.t == 0;
-      const bool two = 2 * at.t + 1 < paged_unit_blocks(a, at.sp);
-      if (first) wait(q_ready, units++);
-      wait(kfull + 8 * stage, use);
-      if (!ok) break;
+    int units = 0, turns[2] = {0, 0};
+    // S of rows 128 q .. of tile i
+    auto scores = [&](int i, int q, int halves) {
+      const int stage = i % ST;
+      if (q == 0) {
+        if (i == 0 || at.t == 0) wait(q_ready, units++);
+        wait(kfull + 8 * stage, i / ST);
+      }
+      if (!ok) return;
       tc_fence_after();
       if (leader) {
-        const uint64_t dk = umma_smem_desc(keys0 + stage * C::TILE_BYTES);
+        const bool two = at.two();
+        const uint64_t dq = umma_smem_desc(smem0 + q * C::TILE_BYTES), dk = umma_smem_desc(keys0 + stage * C::TILE_BYTES);
         const uint32_t idesc_s = idesc | ((two ? 128u : 64u) >> 3) << 17;
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
           const uint64_t off = (uint64_t)(k / 4 * (C::PART_BYTES >> 4) + k % 4 * 2);
-          umma_bf16(tmem + C::S, dq + off, dk + off, idesc_s, k ? 1u : 0u);
+          umma_bf16(tmem + 128 * q, dq + off, dk + off, idesc_s, k ? 1u : 0u);
         }
-        umma_commit(kempty + 8 * stage);
-        umma_commit(s_full);
+        if (q + 1 == halves) umma_commit(kempty + 8 * stage);
+        umma_commit(s_full + 8 * q);
       }
       __syncwarp();
-      wait(p_ready, i);
-      wait(vfull + 8 * stage, use);
-      if (!ok) break;
-      tc_fence_after();
-      if (leader) {
-        const uint64_t dv = umma_smem_desc(values0 + stage * C::TILE_BYTES);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {              // 16 slots: two groups of eight rows, 2 KB
-          if (k >= 4 && !two) break;
-#pragma unroll
-          for (int p = 0; p < PARTS; ++p)
-            umma_bf16_ts(tmem + C::O + 64 * p, tmem + C::S + k / 4 * 64 + k % 4 * 8, dv + (uint64_t)(p * (C::PART_BYTES >> 4) + 128 * k), idesc_o, first && k == 0 ? 0u : 1u);
-        }
-        umma_commit(vempty + 8 * stage);
-        umma_commit(o_full);
+    };
+    int halves = at.halves<QT>(a);
+    for (int q = 0; q < halves; ++q) scores(0, q, halves);
+    for (int i = 0; i < run.count && ok; ++i) {
+      const int stage = i % ST, now = halves;
+      const bool first = i == 0 || at.t == 0, two = at.two(), more = i + 1 < run.count;
+      if (more) {
+        at.next(a, ROWS);
+        halves = at.halves<QT>(a);
       }
-      __syncwarp();
-      at.next(a, ROWS);
+      for (int q = 0; q < QT && ok; ++q) {
+        if (q < now) {
+          wait(p_ready + 8 * q, turns[q]++);
+          if (q == 0) wait(vfull + 8 * stage, i / ST);
+          if (!ok) break;
+          tc_fence_after();
+          if (leader) {
+            const uint64_t dv = umma_smem_desc(values0 + stage * C::TILE_BYTES);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {          // 16 slots: two groups of eight rows, 2 KB
+              if (k >= 4 && !two) break;
+#pragma unroll
+              for (int p = 0; p < PARTS; ++p)
+                umma_bf16_ts(tmem + C::O + D * q + 64 * p, tmem + 128 * q + k / 4 * 64 + k % 4 * 8, dv + (uint64_t)(p * (C::PART_BYTES >> 4) + 128 * k), idesc_o,
+                             first && k == 0 ? 0u : 1u);
+            }
+            if (q + 1 == now) umma_commit(vempty + 8 * stage);
+            umma_commit(o_full + 8 * q);
+          }
+          __syncwarp();
+        }
+        if (more && q < halves) scores(i + 1, q, halves);
+      }
     }
     if (!ok) {                                     // nothing that was issued may outlive the CTA
       if (leader) umma_commit(drained);
@@ -263,154 +333,185 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) tree_attn_tc_kernel(const
     }
   } else {
     // ---------------- softmax
-    const int w4 = warp & 3, part = warp >> 2, row = w4 * 32 + lane;
-    const uint32_t trow = tmem + ((uint32_t)(w4 * 32) << 16), mine = trow + C::S + part * 64;
-    auto meet = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(2 + w4) : "memory"); };
+    const int q = warp >> 3, w4 = warp & 3, part = warp >> 2 & 1, row = w4 * 32 + lane, meeting = 1 + q * 4 + w4;
+    const uint32_t trow = tmem + ((uint32_t)(w4 * 32) << 16), mine = trow + 128 * q + part * 64, sums = trow + C::O + D * q + part * (D / 2);
     const float scale = a.scale2 == 0.f ? 1.f : fabsf(a.scale2);
+    const uint64_t scale2 = f32x2(scale, scale);
     TreeWalk at(a, run, ROWS);
     int2 range = make_int2(0, 0), open = make_int2(0, 0);
-    int token = 0, seg_first = 0, row0 = 0, h = 0, looks = 0;
-    bool live = false, nan_seen = false;
-    float m = -INFINITY, l = 0.f;                  // the reference; the sum of this thread's slots
-    for (int i = 0; i < run.count; ++i) {
+    int token = 0, seg_first = 0, row0 = 0, h = 0, looks = 0, turn = 0;      // turn: tiles of this warp's rows
+    bool live = false, nan_seen = false, idle = false, seen = false;       // seen: a tile held something that the row sees
+    float m = 0.f, l = 0.f;                        // the reference; the sum of this thread's slots
+    for (int i = 0; i < run.count; ++i, at.next(a, ROWS)) {
       const int stage = i % ST, use = i / ST;
       const bool first = i == 0 || at.t == 0;
       if (first) {
         h = at.u % Hkv, row0 = at.u / Hkv * ROWS, seg_first = at.t;
+        idle = q >= at.halves<QT>(a);
+        open = paged_tree_open(a, at.sp, token_of(a, row0), min(at.sp.n_new, token_of(a, min(R, row0 + ROWS) - 1) + 1) - 1);
+        row0 += q * 128;
         token = row0 + row < R ? token_of(a, row0 + row) : a.M;
         live = token < at.sp.n_new;
         range = paged_tree_range(a, at.sp, at.b, token);
-        open = paged_tree_open(a, at.sp, token_of(a, row0), min(at.sp.n_new, token_of(a, min(R, row0 + ROWS) - 1) + 1) - 1);
-        m = -INFINITY, l = 0.f, nan_seen = false;
+        m = 0.f, l = 0.f, nan_seen = seen = false;
       }
-      const bool two = 2 * at.t + 1 < paged_unit_blocks(a, at.sp), here = part == 0 || two;
-      const int base0 = paged_tile_base<true>(a, at.sp, 2 * at.t), base1 = paged_tile_base<true>(a, at.sp, 2 * at.t + 1), base = part ? base1 : base0;
+      const bool two = at.two(), here = part == 0 || two;
+      const int base0 = at.base(0), base1 = at.base(1), base = part ? base1 : base0;
       wait(info + 8 * (i & 3), i >> 2);
-      const unsigned long long valid0 = sh.valid[i & 3][0], valid1 = sh.valid[i & 3][1], valid = part ? valid1 : valid0;
+      const unsigned long long valid0 = sh.valid[i & 3][0], valid1 = sh.valid[i & 3][1];
       const bool open0 = valid0 == ~0ull && base0 >= open.x && base0 + PA_TILE <= open.y, open1 = !two || (valid1 == ~0ull && base1 >= open.x && base1 + PA_TILE <= open.y);
       const bool all = part ? open1 : open0;       // every row sees every slot of this block
-      wait(s_full, i);
-      unsigned long long sees = ~0ull;
-      if (!(open0 && open1)) {
-        sees = here ? valid & paged_tree_bits(a, at.sp, range, at.b, token, base) : 0ull;
-        wait(vfull + 8 * stage, use);
-        // the two threads of a row look at slot `row` of the tile; the warps then wait for one another, like all roles with a limit
-        uint32_t *const found = sh.bad[looks & 1];
-        uint4 *v = reinterpret_cast<uint4 *>(smem + (values0 - smem0) + stage * C::TILE_BYTES + (PARTS == 2 ? part * C::PART_BYTES : 0) + row * 128);
-        constexpr int CH = PARTS == 2 ? 8 : 4;     // 16-byte chunks of a thread
-        const bool behind = !((row < 64 ? valid0 : valid1) >> (row & 63) & 1);
-        if (!behind) {
-          uint32_t bad = 0;                        // (an exponent of all ones carries into its sign)
-#pragma unroll
-          for (int x = 0; x < CH; ++x) {
-            const uint4 w = v[(x + (PARTS == 2 ? 0 : part * 4) + row) & 7];
-            bad |= ((w.x & 0x7f807f80u) + 0x00800080u) | ((w.y & 0x7f807f80u) + 0x00800080u) | ((w.z & 0x7f807f80u) + 0x00800080u) | ((w.w & 0x7f807f80u) + 0x00800080u);
-          }
-          if (bad & 0x80008000u) atomicOr(found + (row >> 5), 1u << (row & 31));
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(looked);
-        wait(looked, looks++);
-        if (tid < 4) sh.bad[looks & 1][tid] = 0;   // (last read before the products of the tile that it was for)
-        const unsigned long long bad = found[2 * part] | (unsigned long long)found[2 * part + 1] << 32;
-        if (behind || (found[row >> 5] >> (row & 31) & 1)) {
-#pragma unroll
-          for (int x = 0; x < CH; ++x) v[(x + (PARTS == 2 ? 0 : part * 4) + row) & 7] = make_uint4(0u, 0u, 0u, 0u);
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        nan_seen |= (sees & bad) != 0;
+      if (idle) {
+        looks += !(open0 && open1);
+        continue;
       }
+      wait(s_full + 8 * q, turn);
+      unsigned long long sees = ~0ull;             // slots of the block that this row sees
+      if (!all) sees = here ? (part ? valid1 : valid0) & paged_tree_bits(a, at.sp, range, at.b, token, base) : 0ull;
       tc_fence_after();
-      float s[64], top = -INFINITY;
-      if (here) {
-        tmem_load32(mine, s);
-        tmem_load32(mine + 32, s + 32);
-        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-        if (a.scale2 <= 0.f) {
+      // f(slots 16 x .. of the block, their scores), hidden ones -inf; the next ones are on their way meanwhile
+      auto each = [&](auto f) {
+        float s[2][16];
+        tmem_load16(mine, s[0]);
 #pragma unroll
-          for (int e = 0; e < 64; ++e) s[e] = a.scale2 < 0.f ? -s[e] : s[e] * 0.f;
+        for (int x = 0; x < 4; ++x) {
+          float(&y)[16] = s[x & 1];
+          tmem_wait16(y);
+          if (x < 3) tmem_load16(mine + 16 * (x + 1), s[(x + 1) & 1]);
+          if (a.scale2 <= 0.f) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) y[e] = a.scale2 < 0.f ? -y[e] : y[e] * 0.f;
+          }
+          if (!all) {
+            const uint32_t bits = (uint32_t)(sees >> 16 * x);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) y[e] = bits >> e & 1 ? y[e] : -INFINITY;
+          }
+          f(x, y);
         }
-        if (!all) {
+      };
+      uint32_t p[32];
+      float top = -INFINITY, sum = 0.f;
+      auto largest = [&](const float (&y)[16], float (&t)[2]) {
 #pragma unroll
-          for (int e = 0; e < 64; ++e) s[e] = sees >> e & 1 ? s[e] : -INFINITY;
+        for (int e = 0; e < 16; e += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(t[e >> 1 & 1]) : "f"(y[e]), "f"(y[e + 1]));
+      };
+      auto exponentials = [&](bool with_top) {
+        const uint64_t minus = f32x2(-m, -m);
+        uint64_t sum2[2] = {0, 0};
+        float t[2] = {-INFINITY, -INFINITY};
+        each([&](int x, const float (&y)[16]) {
+          if (with_top) largest(y, t);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float2 d = unpack2(fma2(f32x2(y[2 * e], y[2 * e + 1]), scale2, minus));
+            const float p0 = flash_ex2(d.x), p1 = flash_ex2(d.y);
+            sum2[e & 1] = add2(sum2[e & 1], f32x2(p0, p1));
+            p[8 * x + e] = pack_bf16x2(p0, p1);
+          }
+        });
+        const float2 both = unpack2(add2(sum2[0], sum2[1]));
+        sum = both.x + both.y;
+        if (with_top) top = fmaxf(t[0], t[1]) * scale;
+      };
+      if (here) exponentials(true);
+      // whether the row's reference moves, by one half of the tile or by both
+      auto moves = [&]() { return top > m + TREE_TC_SLACK || (!seen && top < m - TREE_TC_SLACK && top > -INFINITY); };
+      sh.top[q][part][row] = top;
+      const bool again = bar_any64(meeting, moves());
+      top = fmaxf(top, sh.top[q][part ^ 1][row]);  // (written again only after this warp's next probabilities)
+      if (again) {                                 // (both warps of these rows)
+        float alpha = 1.f;
+        if (moves()) {
+          alpha = seen ? flash_ex2(m - top) : 0.f;
+          m = top;
+          l *= alpha;
         }
-        float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int e = 0; e < 64; e += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(t4[e >> 1 & 3]) : "f"(s[e]), "f"(s[e + 1]));
-        top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * scale;
-      }
-      sh.top[part][row] = top;
-      meet();
-      top = fmaxf(top, sh.top[part ^ 1][row]);       // (written again only after this warp's next probabilities)
-      float alpha = 1.f;
-      if (top > m + TREE_TC_SLACK || (m == -INFINITY && top > m)) {
-        alpha = flash_ex2(m - top);                // (m -inf: 0)
-        m = top;
-        l *= alpha;
-      }
-      if (!first && __any_sync(0xffffffffu, alpha != 1.f)) {
-        wait(o_full, i - 1);
-        tc_fence_after();
+        if (!first && __any_sync(0xffffffffu, alpha != 1.f)) {
+          wait(o_full + 8 * q, turn - 1);
+          tc_fence_after();
 #pragma unroll 1
-        for (int c = 0; c < D / 2; c += 32) {
-          float o[32];
-          tmem_load32(trow + C::O + part * (D / 2) + c, o);
-          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
+          for (int c = 0; c < D / 2; c += 16) {
+            float o[16];
+            tmem_load16(sums + c, o);
+            tmem_wait16(o);
             uint32_t r[16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(o[16 * x + e] * alpha);
-            tmem_st16(trow + C::O + part * (D / 2) + c + 16 * x, r);
+            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(o[e] * alpha);
+            tmem_st16(sums + c, r);
           }
         }
+        if (here) exponentials(false);
       }
+      seen |= top > -INFINITY;
       if (here) {
-        const float ref = m == -INFINITY ? 0.f : -m;
-        const uint64_t minus = f32x2(ref, ref), scale2 = f32x2(scale, scale);
-        uint64_t sum[2] = {0, 0};
+        l += sum;
+        tmem_st16(mine, *reinterpret_cast<uint32_t(*)[16]>(p));
+        tmem_st16(mine + 16, *reinterpret_cast<uint32_t(*)[16]>(p + 16));
+      }
+      if (!(open0 && open1)) {
+        // The two threads of a row of the first 128 look at slot `row` of the tile; all warps wait for theirs, like all roles with a limit.  (The
+        // second 128 rows' products follow the first's.)
+        uint32_t *const found = sh.bad[looks & 3];
+        uint4 *v = reinterpret_cast<uint4 *>(smem + (values0 - smem0) + stage * C::TILE_BYTES + (PARTS == 2 ? part * C::PART_BYTES : 0) + row * 128);
+        constexpr int CH = PARTS == 2 ? 8 : 4;     // 16-byte chunks of a thread
+        const bool behind = !((row < 64 ? valid0 : valid1) >> (row & 63) & 1), open_row = row < 64 ? open0 : open1;
+        if (q == 0) {
+          wait(vfull + 8 * stage, use);
+          if (!behind && !open_row) {
+            uint32_t bad = 0;                      // (an exponent of all ones carries into its sign)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          uint32_t p[16];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float2 d = unpack2(fma2(f32x2(s[32 * x + 2 * e], s[32 * x + 2 * e + 1]), scale2, minus));
-            const float p0 = flash_ex2(d.x), p1 = flash_ex2(d.y);
-            sum[e & 1] = add2(sum[e & 1], f32x2(p0, p1));
-            p[e] = pack_bf16x2(p0, p1);
+            for (int x = 0; x < CH; ++x) {
+              const uint4 w = v[(x + (PARTS == 2 ? 0 : part * 4) + row) & 7];
+              bad |= ((w.x & 0x7f807f80u) + 0x00800080u) | ((w.y & 0x7f807f80u) + 0x00800080u) | ((w.z & 0x7f807f80u) + 0x00800080u) | ((w.w & 0x7f807f80u) + 0x00800080u);
+            }
+            if (bad & 0x80008000u) atomicOr(found + (row >> 5), 1u << (row & 31));
           }
-          tmem_st16(mine + 16 * x, p);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(looked + 8 * (looks & 1));
         }
-        const float2 both = unpack2(add2(sum[0], sum[1]));
-        l += both.x + both.y;
+        wait(looked + 8 * (looks & 1), looks >> 1);
+        const unsigned long long bad = found[2 * part] | (unsigned long long)found[2 * part + 1] << 32;
+        if (q == 0) {
+          // (the one after next: who comes last is one tile behind)
+          if (tid < 4) sh.bad[(looks + 2) & 3][tid] = 0;
+          if (behind || (found[row >> 5] >> (row & 31) & 1)) {
+#pragma unroll
+            for (int x = 0; x < CH; ++x) v[(x + (PARTS == 2 ? 0 : part * 4) + row) & 7] = make_uint4(0u, 0u, 0u, 0u);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        ++looks;
+        nan_seen |= !all && (sees & bad) != 0;
       }
       tmem_stored();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(p_ready);
+      if (lane == 0) mbar_arrive(p_ready + 8 * q);
 
       if (at.t + 1 == at.sp.tiles || i + 1 == run.count) {
         // the unit, or this CTA's part of it, ends
         if (nan_seen) l = NAN;
-        sh.sum[part][row] = l;
-        meet();
-        l = sh.sum[0][row] + sh.sum[1][row];
-        wait(o_full, i);
+        sh.sum[q][part][row] = l;
+        bar_any64(meeting, false);
+        l = sh.sum[q][0][row] + sh.sum[q][1][row];
+        wait(o_full + 8 * q, turn);
         if (!ok) l = NAN;
         tc_fence_after();
         const bool whole = seg_first == 0 && at.t + 1 == at.sp.tiles;
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        float *dst_o = a.part_o + ((long long)(2 * blockIdx.x + (seg_first == 0)) * ROWS + row) * D + part * (D / 2);
+        const long long part_row = (long long)(2 * blockIdx.x + (seg_first == 0)) * ROWS + q * 128 + row;
+        float *dst_o = a.part_o + part_row * D + part * (D / 2);
         bf16 *dst = live ? paged_out_row<bf16>(a, at.b, h, row0 + row, D) + part * (D / 2) : nullptr;
 #pragma unroll 1
-        for (int c = 0; c < D / 2; c += 32) {
-          float o[32];
-          tmem_load32(trow + C::O + part * (D / 2) + c, o);
-          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        for (int c = 0; c < D / 2; c += 16) {
+          float o[16];
+          tmem_load16(sums + c, o);
+          tmem_wait16(o);
           if (whole) {
             if (live) {
 #pragma unroll
-              for (int x = 0; x < 4; ++x) {
+              for (int x = 0; x < 2; ++x) {
                 uint32_t w[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(o[8 * x + 2 * e] * inv, o[8 * x + 2 * e + 1] * inv);
@@ -419,14 +520,14 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) tree_attn_tc_kernel(const
             }
           } else if (row0 + row < R) {
 #pragma unroll
-            for (int x = 0; x < 8; ++x) *reinterpret_cast<float4 *>(dst_o + c + 4 * x) = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+            for (int x = 0; x < 4; ++x) *reinterpret_cast<float4 *>(dst_o + c + 4 * x) = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
           }
         }
         if (part == 0 && whole && live) paged_write_lse(a, at.b, h, row0 + row, m, l);
-        if (part == 0 && !whole && row0 + row < R) a.part_ml[(2 * blockIdx.x + (seg_first == 0)) * ROWS + row] = make_float2(m, l);
+        if (part == 0 && !whole && row0 + row < R) a.part_ml[part_row] = make_float2(l == 0.f ? -INFINITY : m, l);
         tc_fence_before();                         // (the next unit's products wait for this warp's next probabilities)
       }
-      at.next(a, ROWS);
+      ++turn;
     }
   }
   tc_fence_before();

@@ -167,13 +167,17 @@ int paged_args(PagedAttnArgs *a, const PagedPlan &pl, const tsfm_kv_pages *pages
 
 // Maps of the pool for TMA: {element, slot, head, page}, boxes of 128 (64) bytes and up to 64 slots of a page.  False where the driver
 // has no encoder or refuses the pool's strides.
-bool paged_maps(CUtensorMap *k, CUtensorMap *v, const PagesDev &pg, int D, int e) {
+PFN_encodeTiled tensor_map_encoder() {
   static const PFN_encodeTiled encode = [] {
     void *fn = nullptr;
     cudaDriverEntryPointQueryResult res{};
     if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &res) != cudaSuccess || res != cudaDriverEntryPointSuccess) fn = nullptr;
     return (PFN_encodeTiled)fn;
   }();
+  return encode;
+}
+bool paged_maps(CUtensorMap *k, CUtensorMap *v, const PagesDev &pg, int D, int e) {
+  const PFN_encodeTiled encode = tensor_map_encoder();
   if (!encode) return false;
   const cuuint32_t page = 1u << pg.page_log;
   const cuuint64_t dims[4] = {(cuuint64_t)D, page, (cuuint64_t)pg.n_kv_heads, (cuuint64_t)pg.n_pages};

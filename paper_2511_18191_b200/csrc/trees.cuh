@@ -23,9 +23,12 @@ int tree_plan(PagedPlan *pl, PagedPlan *tc, const tsfm_kv_pages *p, int B, int M
   *tc = *pl;
   if (!tree_on_tc(p, M, n_heads)) return TSFM_OK;
   const long long R = (long long)M * (n_heads / p->n_kv_heads), pairs = (long long)B * p->n_kv_heads;
-  tc->rows = 128;
-  tc->chunks = (int)((R + 127) / 128);
-  tc->grid = (int)std::min<long long>(pairs * tc->chunks * ((max_len + 2 * PA_TILE - 1) / (2 * PA_TILE) + 1), 2 * kSms);
+#ifndef TREE_QT2
+#define TREE_QT2 129
+#endif
+  tc->rows = R >= TREE_QT2 ? 256 : 128;
+  tc->chunks = (int)((R + tc->rows - 1) / tc->rows);
+  tc->grid = (int)std::min<long long>(pairs * tc->chunks * ((max_len + 2 * PA_TILE - 1) / (2 * PA_TILE) + 1), (tc->rows == 256 ? 1 : 2) * kSms);
   size_t at = align256(sizeof(PagedMeta) * tc->grid);
   tc->part_ml = at;
   at = align256(at + sizeof(float2) * 2 * tc->grid * tc->rows);
@@ -35,10 +38,22 @@ int tree_plan(PagedPlan *pl, PagedPlan *tc, const tsfm_kv_pages *p, int B, int M
   return TSFM_OK;
 }
 
-template <int D> cudaError_t launch_tree_tc(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl, const CUtensorMap &k, const CUtensorMap &v) {
-  if (cudaError_t e = launch_paged_tiles<TreeTc<D>>(s, a, pl, k, v, tree_attn_tc_kernel<TreeTc<D>>)) return e;
+// Map of the queries: {element, head, token}, boxes of a group's heads x the tokens that make 128 rows.
+bool query_map(CUtensorMap *q, const PagedAttnArgs &a, int D) {
+  if (128 % a.group || a.q_stride * 2 >= 1ll << 40) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)a.n_heads, (cuuint64_t)a.B * a.M}, strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)a.q_stride * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)a.group, (cuuint32_t)(128 / a.group)}, one[3] = {1, 1, 1};
+  return tensor_map_encoder()(q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(a.q), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+template <typename C> cudaError_t launch_tree_tc(cudaStream_t s, const PagedAttnArgs &a, const PagedPlan &pl, const CUtensorMap &k, const CUtensorMap &v) {
+  if (cudaError_t e = cudaFuncSetAttribute(tree_attn_tc_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES)) return e;
+  CUtensorMap q{};
+  const int q_tma = query_map(&q, a, C::D);
+  tree_attn_tc_kernel<C><<<pl.grid, C::THREADS, C::SMEM_BYTES, s>>>(a, k, v, q, q_tma);
+  if (cudaError_t e = cudaGetLastError()) return e;
   LAUNCHED();
-  return join_paged<bf16, D, true>(s, a, pl);
+  return join_paged<bf16, C::D, true>(s, a, pl);
 }
 
 // tsfm_tree_attention (mask or a chain) and tsfm_window_attention
@@ -66,7 +81,9 @@ int tree_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int6
   const int D = pages->d_head;
   cudaError_t err;
   if (pl.rows == 128)
-    err = D == 64 ? launch_tree_tc<64>(s, a, pl, k, v) : launch_tree_tc<128>(s, a, pl, k, v);
+    err = D == 64 ? launch_tree_tc<TreeTc<64, 1>>(s, a, pl, k, v) : launch_tree_tc<TreeTc<128, 1>>(s, a, pl, k, v);
+  else if (pl.rows == 256)
+    err = D == 64 ? launch_tree_tc<TreeTc<64, 2>>(s, a, pl, k, v) : launch_tree_tc<TreeTc<128, 2>>(s, a, pl, k, v);
   else if (pages->dtype == TSFM_BF16)
     err = D == 32 ? launch_paged<bf16, 32, true>(s, a, pl) : D == 64 ? launch_paged<bf16, 64, true>(s, a, pl) : launch_paged<bf16, 128, true>(s, a, pl);
   else
