@@ -42,44 +42,41 @@ struct TreeTcShared {
   uint32_t tmem;
 };
 
-// A CTA's way through its run; every role walks by itself.
+// A CTA's way through its run; every role walks by itself.  Of the unit only what every tile asks for is kept: registers are short, and what the
+// spilled ones cost in every tile was more than all else that is not softmax.
 struct TreeWalk {
-  int b, u, t, len, n_new, len_next, new_next;
+  int b, u, t;
   int blocks, sink, gap;                           // of the unit: its blocks, those with sinks, slots between these and the others
-  PagedSpan sp;
-  __device__ __forceinline__ void unit(const PagedAttnArgs &a) {
-    blocks = paged_unit_blocks(a, sp);
-    sink = paged_sink_tiles(a, sp);
-    gap = (sp.tile0 - sink) * PA_TILE;
+  __device__ __forceinline__ int tiles() const { return (blocks + 1) >> 1; }
+  __device__ __forceinline__ PagedSpan span(const PagedAttnArgs &a, int rows) const { return paged_unit_span<2>(a, b, u / a.pg.n_kv_heads, rows, false); }
+  __device__ __forceinline__ bool enter(const PagedAttnArgs &a, int rows) {        // false: the unit has no live row
+    const PagedSpan s = span(a, rows);
+    blocks = paged_unit_blocks(a, s);
+    sink = paged_sink_tiles(a, s);
+    gap = (s.tile0 - sink) * PA_TILE;
+    return s.tiles;
   }
-  // First slot of block x of the tile; whether it is one.
+  __device__ __forceinline__ TreeWalk(const PagedAttnArgs &a, const PagedRun &run, int rows) : b(run.b), u(run.u), t(run.first) { enter(a, rows); }
+  // (bounded by the series, as paged_next_tile is)
+  __device__ __forceinline__ void next(const PagedAttnArgs &a, int rows) {
+    if (++t < tiles()) return;
+    t = 0;
+    if (++u < a.units && (u % a.pg.n_kv_heads || enter(a, rows))) return;         // (another head's rows of the same chunk, or the next chunk)
+    u = 0;
+    while (b + 1 < a.B) {
+      ++b;
+      if (enter(a, rows)) break;
+    }
+  }
+  // First slot of block x of the tile; whether the second is one.
   __device__ __forceinline__ int base(int x) const {
     const int k = 2 * t + x;
     return k * PA_TILE + (k < sink ? 0 : gap);
   }
   __device__ __forceinline__ bool two() const { return 2 * t + 1 < blocks; }
-  __device__ __forceinline__ void peek(const PagedAttnArgs &a) {
-    const int at = min(b + 1, a.B - 1);
-    len_next = __ldg(a.len + at);
-    new_next = a.n_new ? __ldg(a.n_new + at) : a.M;
-  }
-  __device__ __forceinline__ TreeWalk(const PagedAttnArgs &a, const PagedRun &run, int rows) : b(run.b), u(run.u), t(run.first) {
-    len = __ldg(a.len + b);
-    n_new = a.n_new ? __ldg(a.n_new + b) : a.M;
-    sp = paged_unit_span<2>(a, len, n_new, u / a.pg.n_kv_heads, rows, false);
-    unit(a);
-    peek(a);
-  }
-  __device__ __forceinline__ void next(const PagedAttnArgs &a, int rows) {
-    paged_next_unit_tile<2>(a, rows, b, u, t, sp, len, n_new, [&]() {
-      len = len_next, n_new = new_next;
-      peek(a);
-    });
-    if (t == 0) unit(a);
-  }
   // How many times 128 rows of the unit hold a live one.
-  template <int QT> __device__ __forceinline__ int halves(const PagedAttnArgs &a) const {
-    return QT == 2 && sp.n_new * (long long)a.group - u / a.pg.n_kv_heads * (128ll * QT) > 128 ? 2 : 1;
+  template <int QT> __device__ __forceinline__ int halves(const PagedAttnArgs &a, const PagedSpan &s) const {
+    return QT == 2 && s.n_new * (long long)a.group - u / a.pg.n_kv_heads * (128ll * QT) > 128 ? 2 : 1;
   }
 };
 
@@ -181,6 +178,7 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
     // ---------------- fetches
     const int box_log = min(a.pg.page_log, 6), boxes = PA_TILE >> box_log;
     TreeWalk ahead(a, run, ROWS);                  // the tile whose page ids are looked up; lane 8 h + j: box j of block h
+    PagedSpan span_ahead = ahead.span(a, ROWS);
     int id = 0;                                    // (not looked at before its tile's turn: nothing waits for the load until then)
     bool asked = false;
     int h = 0;
@@ -188,7 +186,7 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
       const int h = lane >> 3, j = lane & 7;
       asked = h < 2 && j < boxes && (h == 0 || ahead.two());
       const int slot = ahead.base(h) + (j << box_log);
-      asked = asked && paged_wants<true>(a, ahead.sp, slot, 1 << box_log);
+      asked = asked && paged_wants<true>(a, span_ahead, slot, 1 << box_log);
       if (asked) id = __ldg(a.pg.table + (long long)ahead.b * a.pg.table_stride + (slot >> a.pg.page_log));
     };
     look_up();
@@ -196,8 +194,10 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
       const int stage = i % ST, use = i / ST, page = asked && (unsigned)id < (unsigned)a.pg.n_pages ? id : -1;
       if (__any_sync(0xffffffffu, asked && page < 0)) pages_report(a.pg, BAD_ID);
       const TreeWalk at = ahead;
+      const PagedSpan span = span_ahead;
       if (i + 1 < run.count) {
         ahead.next(a, ROWS);
+        if (ahead.t == 0) span_ahead = ahead.span(a, ROWS);
         look_up();
       }
       const bool first = i == 0 || at.t == 0;
@@ -211,7 +211,7 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const int s = (x & 1) * 32 + lane;
-        v[x] = __ballot_sync(0xffffffffu, (x < 2 || two) && paged_wants<true>(a, at.sp, base[x >> 1] + s, 1) && (got >> ((x >> 1) * 8 + (s >> box_log)) & 1));
+        v[x] = __ballot_sync(0xffffffffu, (x < 2 || two) && paged_wants<true>(a, span, base[x >> 1] + s, 1) && (got >> ((x >> 1) * 8 + (s >> box_log)) & 1));
       }
       auto issue = [&](uint32_t dst, const CUtensorMap *map, uint32_t bar, int more) {
         if (lane == 0) mbar_expect_tx(bar, __popc(got) * (PARTS * 128 << box_log) + more);
@@ -235,7 +235,7 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
       if (first) {
         if (i) wait(kempty + 8 * ((i - 1) % ST), (i - 1) / ST);          // the queries' last products are done
         if (!ok) break;
-        const int row0 = at.u / Hkv * ROWS, halves = at.halves<QT>(a);
+        const int row0 = at.u / Hkv * ROWS, halves = at.halves<QT>(a, span);
         if (q_tma) {
           if (lane == 0) mbar_expect_tx(q_ready, halves * C::TILE_BYTES);
           __syncwarp();
@@ -293,14 +293,14 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
       }
       __syncwarp();
     };
-    int halves = at.halves<QT>(a);
+    int halves = at.halves<QT>(a, at.span(a, ROWS));
     for (int q = 0; q < halves; ++q) scores(0, q, halves);
     for (int i = 0; i < run.count && ok; ++i) {
       const int stage = i % ST, now = halves;
       const bool first = i == 0 || at.t == 0, two = at.two(), more = i + 1 < run.count;
       if (more) {
         at.next(a, ROWS);
-        halves = at.halves<QT>(a);
+        if (QT == 2 && at.t == 0) halves = at.halves<QT>(a, at.span(a, ROWS));
       }
       for (int q = 0; q < QT && ok; ++q) {
         if (q < now) {
@@ -338,25 +338,24 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
     const float scale = a.scale2 == 0.f ? 1.f : fabsf(a.scale2);
     const uint64_t scale2 = f32x2(scale, scale);
     TreeWalk at(a, run, ROWS);
-    int2 range = make_int2(0, 0), open = make_int2(0, 0);
-    int token = 0, seg_first = 0, row0 = 0, h = 0, looks = 0, turn = 0;      // turn: tiles of this warp's rows
-    bool live = false, nan_seen = false, idle = false, seen = false;       // seen: a tile held something that the row sees
+    int2 open = make_int2(0, 0);
+    int looks = 0, turn = 0;                       // turn: tiles of this warp's rows
+    bool from_start = false, nan_seen = false, idle = false, seen = false;       // seen: a tile held something that the row sees
+    auto row_of = [&]() { return at.u / Hkv * ROWS + q * 128 + row; };
     float m = 0.f, l = 0.f;                        // the reference; the sum of this thread's slots
     for (int i = 0; i < run.count; ++i, at.next(a, ROWS)) {
       const int stage = i % ST, use = i / ST;
       const bool first = i == 0 || at.t == 0;
       if (first) {
-        h = at.u % Hkv, row0 = at.u / Hkv * ROWS, seg_first = at.t;
-        idle = q >= at.halves<QT>(a);
-        open = paged_tree_open(a, at.sp, token_of(a, row0), min(at.sp.n_new, token_of(a, min(R, row0 + ROWS) - 1) + 1) - 1);
-        row0 += q * 128;
-        token = row0 + row < R ? token_of(a, row0 + row) : a.M;
-        live = token < at.sp.n_new;
-        range = paged_tree_range(a, at.sp, at.b, token);
+        const PagedSpan span = at.span(a, ROWS);
+        const int row0 = at.u / Hkv * ROWS;
+        from_start = at.t == 0;
+        idle = q >= at.halves<QT>(a, span);
+        open = paged_tree_open(a, span, token_of(a, row0), min(span.n_new, token_of(a, min(R, row0 + ROWS) - 1) + 1) - 1);
         m = 0.f, l = 0.f, nan_seen = seen = false;
       }
       const bool two = at.two(), here = part == 0 || two;
-      const int base0 = at.base(0), base1 = at.base(1), base = part ? base1 : base0;
+      const int base0 = at.base(0), base1 = at.base(1);
       wait(info + 8 * (i & 3), i >> 2);
       const unsigned long long valid0 = sh.valid[i & 3][0], valid1 = sh.valid[i & 3][1];
       const bool open0 = valid0 == ~0ull && base0 >= open.x && base0 + PA_TILE <= open.y, open1 = !two || (valid1 == ~0ull && base1 >= open.x && base1 + PA_TILE <= open.y);
@@ -367,7 +366,11 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
       }
       wait(s_full + 8 * q, turn);
       unsigned long long sees = ~0ull;             // slots of the block that this row sees
-      if (!all) sees = here ? (part ? valid1 : valid0) & paged_tree_bits(a, at.sp, range, at.b, token, base) : 0ull;
+      if (!all) {
+        const PagedSpan span = at.span(a, ROWS);
+        const int token = row_of() < R ? token_of(a, row_of()) : a.M;
+        sees = here ? (part ? valid1 : valid0) & paged_tree_bits(a, span, paged_tree_range(a, span, at.b, token), at.b, token, part ? base1 : base0) : 0ull;
+      }
       tc_fence_after();
       // f(slots 16 x .. of the block, their scores), hidden ones -inf; the next ones are on their way meanwhile
       auto each = [&](auto f) {
@@ -489,7 +492,7 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
       __syncwarp();
       if (lane == 0) mbar_arrive(p_ready + 8 * q);
 
-      if (at.t + 1 == at.sp.tiles || i + 1 == run.count) {
+      if (at.t + 1 == at.tiles() || i + 1 == run.count) {
         // the unit, or this CTA's part of it, ends
         if (nan_seen) l = NAN;
         sh.sum[q][part][row] = l;
@@ -498,11 +501,12 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
         wait(o_full + 8 * q, turn);
         if (!ok) l = NAN;
         tc_fence_after();
-        const bool whole = seg_first == 0 && at.t + 1 == at.sp.tiles;
+        const int r = row_of(), h = at.u % Hkv;
+        const bool whole = from_start && at.t + 1 == at.tiles(), live = r < R && token_of(a, r) < at.span(a, ROWS).n_new;
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        const long long part_row = (long long)(2 * blockIdx.x + (seg_first == 0)) * ROWS + q * 128 + row;
+        const long long part_row = (long long)(2 * blockIdx.x + from_start) * ROWS + q * 128 + row;
         float *dst_o = a.part_o + part_row * D + part * (D / 2);
-        bf16 *dst = live ? paged_out_row<bf16>(a, at.b, h, row0 + row, D) + part * (D / 2) : nullptr;
+        bf16 *dst = live ? paged_out_row<bf16>(a, at.b, h, r, D) + part * (D / 2) : nullptr;
 #pragma unroll 1
         for (int c = 0; c < D / 2; c += 16) {
           float o[16];
@@ -518,13 +522,13 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
                 *reinterpret_cast<uint4 *>(dst + c + 8 * x) = make_uint4(w[0], w[1], w[2], w[3]);
               }
             }
-          } else if (row0 + row < R) {
+          } else if (r < R) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) *reinterpret_cast<float4 *>(dst_o + c + 4 * x) = make_float4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
           }
         }
-        if (part == 0 && whole && live) paged_write_lse(a, at.b, h, row0 + row, m, l);
-        if (part == 0 && !whole && row0 + row < R) a.part_ml[part_row] = make_float2(l == 0.f ? -INFINITY : m, l);
+        if (part == 0 && whole && live) paged_write_lse(a, at.b, h, r, m, l);
+        if (part == 0 && !whole && r < R) a.part_ml[part_row] = make_float2(l == 0.f ? -INFINITY : m, l);
         tc_fence_before();                         // (the next unit's products wait for this warp's next probabilities)
       }
       ++turn;
