@@ -18,17 +18,16 @@ bool tree_on_tc(const tsfm_kv_pages *p, int M, int n_heads) {
   return p->dtype == TSFM_BF16 && p->d_head >= 64 && p->page_size >= 8 && (long long)M * (n_heads / p->n_kv_heads) >= TREE_TC_MIN_ROWS;
 }
 // Plan of either kernel; pl->bytes: what both would need (a pool's strides, which say whether TMA can read it, are not known here).
-int tree_plan(PagedPlan *pl, PagedPlan *tc, const tsfm_kv_pages *p, int B, int M, int n_heads, int max_len) {
+int tree_plan(PagedPlan *pl, PagedPlan *tc, bool tree, const tsfm_kv_pages *p, int B, int M, int n_heads, int max_len) {
   if (int rc = paged_plan(pl, p, B, M, n_heads, max_len, false)) return rc;
   *tc = *pl;
   if (!tree_on_tc(p, M, n_heads)) return TSFM_OK;
   const long long R = (long long)M * (n_heads / p->n_kv_heads), pairs = (long long)B * p->n_kv_heads;
-#ifndef TREE_QT2
-#define TREE_QT2 129
-#endif
-  tc->rows = R >= TREE_QT2 ? 256 : 128;
+  // A tree's rows all read the same slots: a CTA takes 256 of them beside one another (tree-large of 61 nodes, 4 heads a group: 220 us against 234).  A
+  // chain's chunks have each a window of their own, which more rows make longer (4096 tokens, window 1024: 499 us against 441 with 128).
+  tc->rows = tree && R > 128 ? 256 : 128;
   tc->chunks = (int)((R + tc->rows - 1) / tc->rows);
-  tc->grid = (int)std::min<long long>(pairs * tc->chunks * ((max_len + 2 * PA_TILE - 1) / (2 * PA_TILE) + 1), (tc->rows == 256 ? 1 : 2) * kSms);
+  tc->grid = (int)std::min<long long>(pairs * tc->chunks * ((max_len + 2 * PA_TILE - 1) / (2 * PA_TILE) + 1), 2 * kSms * 128 / tc->rows);
   size_t at = align256(sizeof(PagedMeta) * tc->grid);
   tc->part_ml = at;
   at = align256(at + sizeof(float2) * 2 * tc->grid * tc->rows);
@@ -62,7 +61,7 @@ int tree_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int6
                    int32_t window, int32_t sinks, int32_t max_len, float *lse, void *workspace, size_t workspace_bytes) {
   if (!q || !out || !len || !workspace || window < 0 || sinks < 0 || !std::isfinite(scale * kLog2E)) return TSFM_ERR_ARG;
   PagedPlan pl, tc;
-  if (int rc = tree_plan(&pl, &tc, pages, B, M, n_heads, max_len)) return rc;
+  if (int rc = tree_plan(&pl, &tc, mask != nullptr, pages, B, M, n_heads, max_len)) return rc;
   PagedAttnArgs a{};
   CUtensorMap k{}, v{};
   if (tree_on_tc(pages, M, n_heads)) {
@@ -113,8 +112,9 @@ int tsfm_rope_append_tree(void *stream, const tsfm_rope *rope, const tsfm_kv_pag
 }
 
 size_t tsfm_tree_attention_workspace(const tsfm_kv_pages *pages, int32_t B, int32_t M, int32_t n_heads, int32_t max_len) {
-  PagedPlan pl, tc;
-  return tree_plan(&pl, &tc, pages, B, M, n_heads, max_len) ? 0 : pl.bytes;
+  PagedPlan chain, tree, tc;
+  if (tree_plan(&chain, &tc, false, pages, B, M, n_heads, max_len) || tree_plan(&tree, &tc, true, pages, B, M, n_heads, max_len)) return 0;
+  return std::max(chain.bytes, tree.bytes);
 }
 
 int tsfm_tree_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int64_t q_stride, void *out, int64_t out_stride,
