@@ -17,7 +17,12 @@ struct LogprobArgs {
   float *best;
 };
 
-constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32, LP_UNROLL = 4, LP_MAX_CLUSTER = 8, LP_MAX_TOP = 32, LP_ROOM = 512;
+constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32, LP_MAX_CLUSTER = 8, LP_MAX_TOP = 32, LP_ROOM = 512;
+
+// 16 entries of a thread at a time, the next 16 on their way; CTAs on an SM.
+template <typename T> struct LogprobShape {
+  static constexpr int U = (int)sizeof(T), CTAS = sizeof(T) == 2 ? 5 : 4;        // vectors at a time
+};
 
 // One number for an entry: the larger the logit the larger, among equals the lower the token the larger; never 0.  -0 equals 0, NaN lies below
 // -inf.
@@ -87,6 +92,27 @@ template <int U> __device__ __forceinline__ float largest(const uint4 (&v)[U], f
   return m;
 }
 
+// Two elements as floats, -inf as something finite (NaN stays).
+constexpr float LP_FAR = 1e30f;
+__device__ __forceinline__ float2 finite_logits(const uint4 &v, int i, bf16) {
+  const __nv_bfloat162 far = __float2bfloat162_rn(-LP_FAR);
+  const __nv_bfloat162 y = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162 *>(&(&v.x)[i]), far);
+  const uint32_t w = *reinterpret_cast<const uint32_t *>(&y);
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+__device__ __forceinline__ float2 finite_logits(const uint4 &v, int i, float) {
+  return make_float2(max_or_nan(__uint_as_float((&v.x)[2 * i]), -LP_FAR), max_or_nan(__uint_as_float((&v.x)[2 * i + 1]), -LP_FAR));
+}
+
+// Descending order of a warp's keys that rise and then fall, or the other way round.
+__device__ __forceinline__ unsigned long long warp_merge(unsigned long long key, int lane) {
+#pragma unroll
+  for (int j = 16; j; j >>= 1) {
+    const unsigned long long other = __shfl_xor_sync(0xffffffffu, key, j);
+    if ((key < other) == !(lane & j)) key = other;
+  }
+  return key;
+}
 // Descending order of a warp's keys.
 __device__ __forceinline__ unsigned long long warp_sort(unsigned long long key, int lane) {
 #pragma unroll
@@ -105,9 +131,9 @@ __device__ __forceinline__ unsigned long long warp_sort(unsigned long long key, 
 // while the row streams.  Behind it every thread's largest entry is one key; the n best keys' threads hold all of the n best entries (any
 // other entry lies below n of those keys), and only their columns are looked at again, from L2.
 template <typename T>
-__global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const __grid_constant__ LogprobArgs a) {
+__global__ void __launch_bounds__(LP_THREADS, LogprobShape<T>::CTAS) token_logprobs_kernel(const __grid_constant__ LogprobArgs a) {
   namespace cg = cooperative_groups;
-  constexpr int N = 16 / (int)sizeof(T), U = LP_UNROLL, STEP = LP_THREADS * U;
+  constexpr int N = 16 / (int)sizeof(T), U = LogprobShape<T>::U, STEP = LP_THREADS * U;
   __shared__ LogSum part[LP_WARPS], whole;
   __shared__ unsigned long long keys[LP_WARPS * LP_MAX_TOP], found[LP_ROOM], top[LP_MAX_TOP];
   __shared__ int columns[LP_MAX_TOP], n_found;
@@ -131,59 +157,110 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const __g
     }
     return r;
   };
-  float m = -INFINITY;
-  uint64_t s2[2] = {0, 0}, t2[2] = {0, 0};
-  int from = -1;                                   // the batch with the largest logit
-  const uint64_t scale = f32x2(a.scale2, a.scale2);
-  for (int v = v0 + tid; v < v1; v += STEP) {
-    uint4 r[U];
+  float m = -INFINITY;                             // the largest logit so far above -1e30
+  int from = -1;                                   // the batch that holds it
+  LogSum mine;
+  bool extreme = a.scale2 >= 1e6f;                 // a maximum, or a scale, with which y scale2 - m scale2 could overflow
+  {
+    float ref = 0.f;                               // m scale2 as rounded
+    float ss[2] = {0.f, 0.f}, tt[2] = {0.f, 0.f};
+    uint4 r[U], next[U];
 #pragma unroll
-    for (int j = 0; j < U; ++j) r[j] = load(v + j * LP_THREADS);
-    const float big = largest(r, T());
-    if (big > m) {
-      const float d = m == -INFINITY ? 0.f : max_or_nan((m - big) * a.scale2, -300.f), f = m == -INFINITY ? 1.f : lp_ex2(d);
-      const float2 s0 = unpack2(s2[0]), s1 = unpack2(s2[1]), t0 = unpack2(t2[0]), t1 = unpack2(t2[1]);
-      const float s = (s0.x + s0.y) + (s1.x + s1.y), t = (t0.x + t0.y) + (t1.x + t1.y);
-      s2[0] = f32x2(s * f, 0.f), t2[0] = f32x2(f * fmaf(s, d, t), 0.f);
-      s2[1] = t2[1] = 0;
-      m = big, from = v;
+    for (int j = 0; j < U; ++j) next[j] = load(v0 + tid + j * LP_THREADS);
+    for (int v = v0 + tid; v < v1; v += STEP) {
+#pragma unroll
+      for (int j = 0; j < U; ++j) r[j] = next[j];
+      if (v + STEP < v1) {
+#pragma unroll
+        for (int j = 0; j < U; ++j) next[j] = load(v + STEP + j * LP_THREADS);
+      }
+      const float big = largest(r, T());
+      if (big > m && big > -LP_FAR) {
+        const float now = big * a.scale2, d = ref - now, f = m == -INFINITY ? 0.f : lp_ex2(d);
+        // (before the first number the sums are 0, or NaN)
+        const float s = ss[0] + ss[1], t = tt[0] + tt[1];
+        ss[0] = m == -INFINITY ? s : s * f, tt[0] = m == -INFINITY ? t : f == 0.f ? 0.f * t : f * fmaf(s, d, t);
+        ss[1] = tt[1] = 0.f;
+        m = big, ref = now, from = v;
+        extreme |= big >= LP_FAR;
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j)
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+          const float2 y = finite_logits(r[j], i, T());
+          const float d0 = fmaf(y.x, a.scale2, -ref), d1 = fmaf(y.y, a.scale2, -ref);
+          const float e0 = lp_ex2(d0), e1 = lp_ex2(d1);
+          ss[0] += e0, ss[1] += e1;
+          tt[0] = fmaf(e0, d0, tt[0]), tt[1] = fmaf(e1, d1, tt[1]);
+        }
     }
+    // against m itself, not against its rounded product
+    const float s = ss[0] + ss[1], t = tt[0] + tt[1];
+    const float off = m == -INFINITY ? 0.f : fmaf(m, a.scale2, -ref), f = exp2f(-off);
+    mine = LogSum{m, s * f, fmaf(-off, s, t) * f};
+  }
+  const bool far = __syncthreads_or(extreme) || !__syncthreads_or(from >= 0);
+  if (far) {                                       // logits beyond 1e30, or none above -1e30: once more, the difference first
+    uint64_t s2 = 0, t2 = 0;
+    m = -INFINITY;
+    for (int v = v0 + tid; v < v1; v += LP_THREADS) {
+      const uint4 r[1] = {load(v)};
+      m = fmaxf(m, largest(r, T()));
+    }
+    from = -1;
     const float ref = m == -INFINITY ? 0.f : -m;
-    const uint64_t minus = f32x2(ref, ref);
-#pragma unroll
-    for (int j = 0; j < U; ++j)
+    for (int v = v0 + tid; v < v1; v += LP_THREADS) {
+      const uint4 r = load(v);
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) {
-        const float2 y = logits_of(r[j], i, T());
-        float2 d = unpack2(mul2(add2(f32x2(y.x, y.y), minus), scale));
+        const float2 y = logits_of(r, i, T());
+        float2 d = unpack2(mul2(add2(f32x2(y.x, y.y), f32x2(ref, ref)), f32x2(a.scale2, a.scale2)));
         d.x = max_or_nan(d.x, -300.f), d.y = max_or_nan(d.y, -300.f);    // (2^-300 is 0, and -inf times it must be too)
         const uint64_t e = f32x2(lp_ex2(d.x), lp_ex2(d.y));
-        s2[i & 1] = add2(s2[i & 1], e);
-        t2[i & 1] = fma2(e, f32x2(d.x, d.y), t2[i & 1]);
+        s2 = add2(s2, e);
+        t2 = fma2(e, f32x2(d.x, d.y), t2);
       }
+    }
+    const float2 s = unpack2(s2), t = unpack2(t2);
+    mine = LogSum{m, s.x + s.y, t.x + t.y};
   }
   {
-    const float2 s0 = unpack2(s2[0]), s1 = unpack2(s2[1]), t0 = unpack2(t2[0]), t1 = unpack2(t2[1]);
-    LogSum mine{m, (s0.x + s0.y) + (s1.x + s1.y), (t0.x + t0.y) + (t1.x + t1.y)};
 #pragma unroll
     for (int o = 16; o; o >>= 1)
       mine = log_sum_join(mine, LogSum{__shfl_xor_sync(0xffffffffu, mine.m, o), __shfl_xor_sync(0xffffffffu, mine.s, o), __shfl_xor_sync(0xffffffffu, mine.t, o)}, a.scale2);
     if (lane == 0) part[warp] = mine;
   }
+  unsigned long long best = 0;
   if (n) {
     // this thread's best entry
     unsigned long long key = 0;
-    const int begin = from >= 0 ? from : v0 + tid, end = from >= 0 ? min(v1, from + STEP) : v1;        // (nothing above -inf: all of them)
-    for (int v = begin; v < end; v += LP_THREADS) {
-      const uint4 r = load(v);
+    if (from >= 0) {
+      int id = 0;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int id = v * N - shift + i;
-        if (id >= 0 && id < V) key = max(key, logit_key(to_f32(reinterpret_cast<const T *>(&r)[i]), id));
+      for (int j = U - 1; j >= 0; --j) {
+        const uint4 r = load(from + j * LP_THREADS);
+#pragma unroll
+        for (int i = N / 2 - 1; i >= 0; --i) {
+          const float2 y = logits_of(r, i, T());
+          const int at = (from + j * LP_THREADS) * N - shift + 2 * i;
+          id = y.x == m ? at : y.y == m ? at + 1 : id;
+        }
+      }
+      key = logit_key(m, id);
+    } else {                                       // (nothing above -inf: all of them)
+      for (int v = v0 + tid; v < v1; v += LP_THREADS) {
+        const uint4 r = load(v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int id = v * N - shift + i;
+          if (id >= 0 && id < V) key = max(key, logit_key(to_f32(reinterpret_cast<const T *>(&r)[i]), id));
+        }
       }
     }
     key = warp_sort(key, lane);
-    if (lane < n) keys[warp * n + lane] = key;
+    best = key;
+    keys[warp * 32 + lane] = key;
     if (tid < LP_MAX_TOP) columns[tid] = -1, top[tid] = 0;
     if (tid == 0) n_found = 0;
   }
@@ -201,21 +278,29 @@ __global__ void __launch_bounds__(LP_THREADS, 4) token_logprobs_kernel(const __g
       for (int i = 0; i < count; ++i) above += list[i] > key;
       return above;
     };
+    // the warps' lists become one: the larger of one from the top and the other from the bottom are the best 32, rising and falling
     __shared__ unsigned long long least;
-    if (tid < LP_WARPS * n && keys[tid]) {
-      const int at = place(keys, LP_WARPS * n, keys[tid]);
-      if (at < n) columns[at] = ((key_id(keys[tid]) + shift) / N - v0) % LP_THREADS;
-      if (at == n - 1) least = keys[tid];
+#pragma unroll
+    for (int w = LP_WARPS / 2; w; w >>= 1) {
+      if (warp < w) keys[warp * 32 + lane] = best = warp_merge(max(best, keys[(warp + w) * 32 + 31 - lane]), lane);
+      __syncthreads();
+    }
+    if (warp == 0 && lane < n) {
+      if (best) columns[lane] = ((key_id(best) + shift) / N - v0) % LP_THREADS;
+      if (lane == n - 1) least = best;
     }
     __syncthreads();
-    const unsigned long long bar = columns[n - 1] >= 0 ? least : 1;      // (fewer keys than n: everything counts)
+    const unsigned long long bar = max(least, 1ull);                     // (fewer keys than n: everything counts)
+    const float low = key_logit(bar);                                    // (NaN: below everything)
     for (int k = warp; k < n && columns[k] >= 0; k += LP_WARPS)
       for (int v = v0 + columns[k] + lane * LP_THREADS; v < v1; v += 32 * LP_THREADS) {
         const uint4 r = load(v);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
+          const float y = to_f32(reinterpret_cast<const T *>(&r)[i]);
+          if (y < low) continue;
           const int id = v * N - shift + i;
-          const unsigned long long key = id >= 0 && id < V ? logit_key(to_f32(reinterpret_cast<const T *>(&r)[i]), id) : 0;
+          const unsigned long long key = id >= 0 && id < V ? logit_key(y, id) : 0;
           if (key >= bar) {
             const int at = atomicAdd(&n_found, 1);
             if (at < LP_ROOM) found[at] = key;

@@ -155,9 +155,9 @@ int tsfm_token_logprobs(void *stream, const void *logits, int64_t stride, int32_
   a.n_top = n_top;
   a.ids = top_ids;
   a.best = top_logprob;
-  // few rows are shared by CTAs, of a batch of loads for each thread at least
+  // few rows are shared by CTAs, of 16 entries for each thread at least
   int cluster = 1;
-  while (cluster < LP_MAX_CLUSTER && 2ll * rows * cluster <= 4 * kSms && (long long)V * e > (long long)cluster * LP_THREADS * LP_UNROLL * 16) cluster *= 2;
+  while (cluster < LP_MAX_CLUSTER && 2ll * rows * cluster <= 4 * kSms && V > (long long)cluster * LP_THREADS * 16) cluster *= 2;
   if ((long long)rows * cluster > kMaxGridX) return TSFM_ERR_SHAPE;
   auto launch = [&](auto kernel) { return launch_cluster((cudaStream_t)stream, (unsigned)(rows * cluster), LP_THREADS, 0, cluster, kernel, a); };
   CU_TRY(dtype == TSFM_BF16 ? launch(token_logprobs_kernel<bf16>) : launch(token_logprobs_kernel<float>));
