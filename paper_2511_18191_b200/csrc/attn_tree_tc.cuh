@@ -538,9 +538,12 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
   __syncthreads();
   if (warp == C::WARPS) {                          // copies that gave no sign get another limit each
     if (!ok)
-      for (int s = 0; s < ST; ++s) {
-        tile_arrived(kfull + 8 * s, 0, a.wait_ns);
-        tile_arrived(kfull + 8 * s, 1, a.wait_ns);
+      for (int phase = 0; phase < 2; ++phase) {
+        for (int s = 0; s < ST; ++s) {
+          tile_arrived(kfull + 8 * s, phase, a.wait_ns);
+          tile_arrived(vfull + 8 * s, phase, a.wait_ns);
+        }
+        tile_arrived(q_ready, phase, a.wait_ns);
       }
   } else if (warp == C::WARPS + 1) {
     tc_fence_after();

@@ -165,8 +165,7 @@ int paged_args(PagedAttnArgs *a, const PagedPlan &pl, const tsfm_kv_pages *pages
   return TSFM_OK;
 }
 
-// Maps of the pool for TMA: {element, slot, head, page}, boxes of 128 (64) bytes and up to 64 slots of a page.  False where the driver
-// has no encoder or refuses the pool's strides.
+// The driver's encoder of maps for TMA, or NULL.
 PFN_encodeTiled tensor_map_encoder() {
   static const PFN_encodeTiled encode = [] {
     void *fn = nullptr;
@@ -176,6 +175,8 @@ PFN_encodeTiled tensor_map_encoder() {
   }();
   return encode;
 }
+// Maps of the pool for TMA: {element, slot, head, page}, boxes of 128 (64) bytes and up to 64 slots of a page.  False where the driver
+// has no encoder or refuses the pool's strides.
 bool paged_maps(CUtensorMap *k, CUtensorMap *v, const PagesDev &pg, int D, int e) {
   const PFN_encodeTiled encode = tensor_map_encoder();
   if (!encode) return false;

@@ -10,10 +10,10 @@ namespace {
 
 static_assert(TREE_MAX == TSFM_MAX_TREE && LP_MAX_TOP == TSFM_MAX_TOP, "as include/tsfm.h says");
 
-#ifndef TREE_TC_MIN_ROWS
-#define TREE_TC_MIN_ROWS 33
-#endif
-// Whether the rows of a key head go to tree_attn_tc_kernel, as far as shapes say.
+// Whether the rows of a key head go to tree_attn_tc_kernel, as far as shapes say: from 17 on.  (It takes 128 at a time, the other kernel 8, 16 or 32.  64 x 20 heads
+// of 64, 346 slots: 16 rows 54 us there, 44 in the other kernel; 17 rows 55 and 63; 33 rows 57 and 100.  16 x 8 heads of 128, 4096 slots: 16 rows 53 and
+// 51, 17 rows 54 and 78, 64 rows 61 and 132.)
+constexpr int TREE_TC_MIN_ROWS = 17;
 bool tree_on_tc(const tsfm_kv_pages *p, int M, int n_heads) {
   return p->dtype == TSFM_BF16 && p->d_head >= 64 && p->page_size >= 8 && (long long)M * (n_heads / p->n_kv_heads) >= TREE_TC_MIN_ROWS;
 }

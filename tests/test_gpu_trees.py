@@ -632,3 +632,136 @@ def test_calls_on_two_streams_at_once():
             call(i, streams[i].cuda_stream)
         torch.cuda.synchronize()
         assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+
+
+# ------------------------------------------------------------------------------------------ what ordinary inputs do not reach
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D,Hq,M", [(64, 4, 5), (64, 8, 40), (128, 16, 40), (128, 8, 70)])
+@pytest.mark.parametrize("kind", ["spread", "low", "high", "rising"])
+def test_scores_far_from_ordinary(dtype, D, Hq, M, kind):
+    """Maxima that move by hundreds from tile to tile, scores that all lie far below or above 0."""
+    lengths = [0, 70, 300]
+    pool = Pool(3, 2, D, 16, [n + M for n in lengths], dtype, seed=8)
+    trees = [tr.tree("random", M, b) for b in range(3)]
+    if kind in ("low", "high"):
+        pool.k[..., 0] = -40.0 if kind == "low" else 40.0
+    if kind == "rising":                                       # the later a slot the larger its scores
+        for b, n in enumerate(lengths):
+            for s in range(n + M):
+                pool.k[pool.table[b, s // 16].long(), :, s % 16, 0] = s / 4.0
+    q = wide((3, M), Hq * D, dtype, 0, 2, 30.0 if kind == "spread" else 1.0)
+    if kind != "spread":
+        q.view(3, M, Hq, D)[..., 0] = 60.0
+    tsfm = lib()
+    for masks in ([tr.ancestors(t) for t in trees], None):
+        out, lse = torch.zeros_like(q), torch.zeros(3, M, Hq, device="cuda")
+        pages, ws = pool.describe(tsfm), torch.empty(1 << 25, dtype=torch.uint8, device="cuda")
+        args = (stream(), pages, q, q.stride(1), out, out.stride(1), ints(lengths), None)
+        if masks:
+            tsfm.tsfm_tree_attention(*args, torch.stack([tr.words(s) for s, _ in masks]).cuda(), ints(np.stack([d for _, d in masks])), False, 3, M, Hq, 0.125, 0, 0,
+                                     300 + M, lse, ws, ws.numel())
+        else:
+            tsfm.tsfm_window_attention(*args, 3, M, Hq, 0.125, 90, 4, 300 + M, lse, ws, ws.numel())
+        for b, n in enumerate(lengths):
+            k, v = pool.rows(pool.k, b, n + M), pool.rows(pool.v, b, n + M)
+            for m in range(0, M, 3):
+                seen = tr.visible(n, M, m, 0, 0, *masks[b]) if masks else tr.visible(n, M, m, 90, 4)
+                o, z, absv, peak, count = tr.attention(q[b, m].cpu().double().view(Hq, D), k, v, 0.125, seen)
+                rel = ref.attention_tolerance(dtype, D, count, peak)[:, None]
+                assert ((out[b, m].cpu().double().view(Hq, D) - o).abs() <= U[dtype] * o.abs() + rel * absv + 1e-30).all(), (b, m)
+                assert ((lse[b, m].cpu().double() - z).abs() <= rel[:, 0] + 4 * U[F32] * (z.abs() + peak + 1)).all(), (b, m)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M", [5, 40])
+@pytest.mark.parametrize("scale", [0.0, -0.125, 3.0])
+def test_any_scale(dtype, M, scale):
+    pool = Pool(2, 2, 64, 16, [100 + M, M], dtype, seed=9)
+    trees = [tr.tree("random", M, b) for b in range(2)]
+    for b, n in enumerate([100, 0]):
+        stale(pool, b, n + M)
+    check(pool, dtype, 8, 2, 64, [100, 0], [M, M], M, trees, scale=scale, window=30, sinks=2)
+    check(pool, dtype, 8, 2, 64, [100, 0], [M, M], M, None, scale=scale)
+
+
+@pytest.mark.parametrize("M", [5, 60])
+def test_depths_are_cut(M):
+    rng = np.random.default_rng(1)
+    lengths = [100, 30]
+    masks, cut = [], []
+    for b in range(2):
+        sees, _ = tr.ancestors(tr.tree("random", M, b))
+        depth = rng.choice([-5, -2 ** 31, 2 ** 31 - 1, M, 1], M)
+        masks.append((sees, depth))
+        cut.append((sees, np.clip(depth, 0, M - 1)))
+    pool = Pool(2, 2, 64, 16, [n + M for n in lengths], BF16, seed=1)
+    a = check(pool, BF16, 8, 2, 64, lengths, [M, M], M, masks=cut, window=20, sinks=1)
+    tsfm = lib()
+    q = wide((2, M), 8 * 64, BF16, 0, 1, 2.0)                  # as check() makes them
+    out, ws = torch.zeros_like(q), torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    tsfm.tsfm_tree_attention(stream(), pool.describe(tsfm), q, q.stride(1), out, out.stride(1), ints(lengths), None, torch.stack([tr.words(s) for s, _ in masks]).cuda(),
+                             ints(np.stack([d for _, d in masks])), False, 2, M, 8, 0.125, 20, 1, max(lengths) + M, None, ws, ws.numel())
+    assert torch.equal(out, a[0][..., :8 * 64])
+
+
+@pytest.mark.parametrize("M,Hq,D,page", [(1, 4, 64, 16), (40, 8, 64, 16), (40, 8, 128, 64), (70, 16, 128, 8)])
+def test_a_wait_that_runs_out_ends_the_call(M, Hq, D, page):
+    """Waits for more bytes than are copied (nothing faults, the copies themselves arrive): the status says so, NaN where it matters, and the next call is
+    whole again."""
+    tsfm = lib()
+    lengths = [500, 200]
+    pool = Pool(2, 2, D, page, [n + M for n in lengths], BF16, seed=3)
+    q = wide((2, M), Hq * D, BF16, 0, 1)
+    pages = pool.describe(tsfm)
+    size = tsfm.tsfm_tree_attention_workspace(pages, 2, M, Hq, 500 + M)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+
+    def run():
+        out = torch.zeros_like(q)
+        tsfm.tsfm_window_attention(stream(), pages, q, q.stride(1), out, out.stride(1), ints(lengths), None, 2, M, Hq, 0.125, 0, 0, 500 + M, None, ws, size)
+        torch.cuda.synchronize()
+        return out
+
+    good = run()
+    try:
+        tsfm.tsfm_debug_tile_wait(2000, 0)
+        bad = run()
+    finally:
+        tsfm.tsfm_debug_tile_wait()
+    assert int(pool.status) == tsfm.TSFM_PAGES_TIMEOUT and torch.isnan(bad.float()).all()
+    pool.status.zero_()
+    assert torch.equal(run(), good) and int(pool.status) == 0
+
+
+def test_a_captured_call_follows_new_lengths_and_trees():
+    """What a graph replays reads lengths, counts, masks and tables as they are then."""
+    tsfm = lib()
+    M, Hq, D = 40, 8, 64
+    pool = Pool(2, 2, D, 16, [400, 400], BF16, seed=3)
+    q = wide((2, M), Hq * D, BF16, 0, 1)
+    pages = pool.describe(tsfm)
+    size = tsfm.tsfm_tree_attention_workspace(pages, 2, M, Hq, 400)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    length, new = ints([10, 300]), ints([M, M])
+    parent = ints([tr.tree("random", M, b) for b in range(2)])
+    mask, depth = torch.zeros(2, M, 1, dtype=torch.int64, device="cuda"), torch.zeros(2, M, dtype=torch.int32, device="cuda")
+    out = torch.zeros_like(q)
+
+    def call(to, work):
+        tsfm.tsfm_tree_init(stream(), parent, new, 2, M, 0, mask, depth)
+        tsfm.tsfm_tree_attention(stream(), pages, q, q.stride(1), to, to.stride(1), length, new, mask, depth, False, 2, M, Hq, 0.125, 50, 2, 400, None, work, size)
+
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        call(out, ws)
+    for lengths, counts, seed in (([10, 300], [M, M], 0), ([0, 350], [7, 0], 5), ([359, 1], [M, 33], 9)):
+        length.copy_(ints(lengths))
+        new.copy_(ints(counts))
+        parent.copy_(ints([tr.tree("random", M, seed + b) for b in range(2)]))
+        out.fill_(-3)
+        graph.replay()
+        want = torch.full_like(out, -3)
+        call(want, torch.empty_like(ws))
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
