@@ -184,6 +184,7 @@ __global__ void __launch_bounds__(LP_THREADS, LogprobShape<T>::CTAS) token_logpr
         m = big, ref = now, from = v;
         extreme |= big >= LP_FAR;
       }
+      float bs[2] = {0.f, 0.f}, bt[2] = {0.f, 0.f};        // (of the batch: shorter sums lose less)
 #pragma unroll
       for (int j = 0; j < U; ++j)
 #pragma unroll
@@ -191,9 +192,10 @@ __global__ void __launch_bounds__(LP_THREADS, LogprobShape<T>::CTAS) token_logpr
           const float2 y = finite_logits(r[j], i, T());
           const float d0 = fmaf(y.x, a.scale2, -ref), d1 = fmaf(y.y, a.scale2, -ref);
           const float e0 = lp_ex2(d0), e1 = lp_ex2(d1);
-          ss[0] += e0, ss[1] += e1;
-          tt[0] = fmaf(e0, d0, tt[0]), tt[1] = fmaf(e1, d1, tt[1]);
+          bs[0] += e0, bs[1] += e1;
+          bt[0] = fmaf(e0, d0, bt[0]), bt[1] = fmaf(e1, d1, bt[1]);
         }
+      ss[0] += bs[0], ss[1] += bs[1], tt[0] += bt[0], tt[1] += bt[1];
     }
     // against m itself, not against its rounded product
     const float s = ss[0] + ss[1], t = tt[0] + tt[1];
