@@ -412,7 +412,7 @@ int tsfm_rope_append(void *stream, const tsfm_rope *rope, const tsfm_kv_pages *p
  * beyond rounding, and are the same each time for the same call.
  * Made for few new tokens: every 8 to 32 (fp32: 1 to 16) of a key head's M n_heads / n_kv_heads rows read all slots that any
  * token of the series sees, also where they belong to tokens m >= n_new[b].  A prompt of thousands of tokens is right but slow
- * (2048 tokens, 32 heads of 128 over 8 key heads: 0.8 ms). */
+ * (2048 tokens, 32 heads of 128 over 8 key heads: 0.8 ms): tsfm_window_attention, with window 0 if there is none, is made for those. */
 int tsfm_paged_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int64_t q_stride, void *out, int64_t out_stride,
                          const int32_t *len, const int32_t *n_new, int32_t B, int32_t M, int32_t n_heads, float scale,
                          int32_t causal, int32_t window, int32_t max_len, float *lse, const float *w_in, float *w_out,
@@ -502,7 +502,9 @@ int tsfm_rope_append_tree(void *stream, const tsfm_rope *rope, const tsfm_kv_pag
  *   depth    [B, M] or [M], cut to 0 .. M - 1; may be NULL with window 0
  *   max_len  the longest series in slots, new ones included: lengths are cut to it.  It sizes the grid and the workspace, not the work
  *   workspace  256-byte aligned, tsfm_tree_attention_workspace() bytes; contents do not matter
- * Head layouts, precision, rows that see nothing, hidden slots, rows behind n_new, lse and status: as tsfm_paged_attention.
+ * Head layouts, rows that see nothing, hidden slots, rows behind n_new, lse and status: as tsfm_paged_attention.  Precision: fp32 scores, exponentials and sums;
+ * out is rounded once, and with bf16 and more than 16 rows of a key head (M n_heads / n_kv_heads) probabilities enter the product with the values as bf16: out may
+ * be off by 2^-8 of the sum of p |v| besides.  There |v| above 2^100 may overflow.  A series' queries behind n_new may hold anything.
  * M <= TSFM_MAX_TREE. */
 int tsfm_tree_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int64_t q_stride, void *out, int64_t out_stride,
                         const int32_t *len, const int32_t *n_new, const uint64_t *mask, const int32_t *depth, int32_t shared_tree, int32_t B,
