@@ -41,7 +41,7 @@ template <int D_, int QT_> struct TreeTc {
 constexpr float TREE_TC_SLACK = 20.f;              // powers of two between a row's maximum and its reference
 
 struct TreeTcShared {
-  unsigned long long kfull[2], kempty[2], vfull[2], vempty[2], info[4], s_full[2], p_ready[2], o_full[2], looked[2], q_ready, drained;
+  unsigned long long kfull[2], kempty[2], vfull[2], vempty[2], info[4], taken[4], s_full[2], p_ready[2], o_full[2], looked[2], q_ready, drained;
   unsigned long long valid[4][2];                  // of a tile's blocks: slots that exist
   float top[2][2][128], sum[2][2][128];            // what the two threads of a row exchange
   uint32_t bad[4][4];                              // slots of such a tile whose values are not finite
@@ -128,7 +128,7 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
   const uint32_t smem0 = (smem_u32(paged_smem_raw) + 1023u) & ~1023u;
   unsigned char *const smem = paged_smem_raw + (smem0 - smem_u32(paged_smem_raw));
   const uint32_t keys0 = smem0 + QT * C::TILE_BYTES, values0 = keys0 + ST * C::TILE_BYTES;
-  const uint32_t kfull = smem_u32(sh.kfull), kempty = smem_u32(sh.kempty), vfull = smem_u32(sh.vfull), vempty = smem_u32(sh.vempty), info = smem_u32(sh.info);
+  const uint32_t kfull = smem_u32(sh.kfull), kempty = smem_u32(sh.kempty), vfull = smem_u32(sh.vfull), vempty = smem_u32(sh.vempty), info = smem_u32(sh.info), taken = smem_u32(sh.taken);
   const uint32_t q_ready = smem_u32(&sh.q_ready), s_full = smem_u32(sh.s_full), p_ready = smem_u32(sh.p_ready), o_full = smem_u32(sh.o_full),
                  looked = smem_u32(sh.looked), drained = smem_u32(&sh.drained);
   const int R = a.M * a.group;
@@ -155,7 +155,10 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
       mbar_init(o_full + 8 * lane, 1);
       mbar_init(looked + 8 * lane, 8);
     }
-    if (lane < 4) mbar_init(info + 8 * lane, 1);
+    if (lane < 4) {
+      mbar_init(info + 8 * lane, 1);
+      mbar_init(taken + 8 * lane, C::WARPS);
+    }
     if (lane < 16) (&sh.bad[0][0])[lane] = 0;
     if (lane == 0) {
       mbar_init(q_ready, 1);
@@ -231,6 +234,8 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
         __syncwarp();
       };
       if (i >= ST) wait(kempty + 8 * stage, use - 1);
+      // (warps without rows in this unit have no part in its products: nothing else holds the ring back for them)
+      if (i >= 4) wait(taken + 8 * (i & 3), (i >> 2) - 1);
       if (!ok) break;
       if (lane == 0) {
         sh.valid[i & 3][0] = v[0] | (unsigned long long)v[1] << 32;
@@ -364,6 +369,8 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
       const int base0 = at.base(0), base1 = at.base(1);
       wait(info + 8 * (i & 3), i >> 2);
       const unsigned long long valid0 = sh.valid[i & 3][0], valid1 = sh.valid[i & 3][1];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(taken + 8 * (i & 3));
       const bool open0 = valid0 == ~0ull && base0 >= open.x && base0 + PA_TILE <= open.y, open1 = !two || (valid1 == ~0ull && base1 >= open.x && base1 + PA_TILE <= open.y);
       const bool all = part ? open1 : open0;       // every row sees every slot of this block
       if (idle) {
