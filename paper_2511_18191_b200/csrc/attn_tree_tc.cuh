@@ -175,6 +175,7 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
   tc_fence_after();
   const uint32_t tmem = sh.tmem;
   bool ok = true;
+  int keys = 0, values = 0, queries = 0;           // (of the warp that fetches) copies that it has asked for
   // a bounded wait of a whole warp; one that ran out is reported, and there are no more
   auto wait = [&](uint32_t bar, int phase) {
     if (ok && __any_sync(0xffffffffu, !tile_arrived(bar, (uint32_t)phase & 1, a.wait_ns))) {
@@ -243,6 +244,7 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
         mbar_arrive(info + 8 * (i & 3));
       }
       issue(keys0 + stage * C::TILE_BYTES, &mapK, kfull + 8 * stage, i >= a.miss_from ? 16 : 0);
+      keys = i + 1;
       if (first) {
         if (i) wait(kempty + 8 * ((i - 1) % ST), (i - 1) / ST);          // the queries' last products are done
         if (!ok) break;
@@ -270,10 +272,12 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
           __syncwarp();
           if (lane == 0) mbar_arrive(q_ready);
         }
+        ++queries;
       }
       if (i >= ST) wait(vempty + 8 * stage, use - 1);
       if (!ok) break;
       issue(values0 + stage * C::TILE_BYTES, &mapV, vfull + 8 * stage, 0);
+      values = i + 1;
     }
   } else if (warp == C::WARPS + 1) {
     // ---------------- products (the warp as a whole, one lane issues)
@@ -336,11 +340,6 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
         }
         if (more && q < halves) scores(i + 1, q, halves);
       }
-    }
-    if (!ok) {                                     // nothing that was issued may outlive the CTA
-      if (leader) umma_commit(drained);
-      __syncwarp();
-      tile_arrived(drained, 0, a.wait_ns);
     }
   } else {
     // ---------------- softmax
@@ -548,17 +547,21 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
     }
   }
   tc_fence_before();
-  __syncthreads();
-  if (warp == C::WARPS) {                          // copies that gave no sign get another limit each
-    if (!ok)
-      for (int phase = 0; phase < 2; ++phase) {
-        for (int s = 0; s < ST; ++s) {
-          tile_arrived(kfull + 8 * s, phase, a.wait_ns);
-          tile_arrived(vfull + 8 * s, phase, a.wait_ns);
-        }
-        tile_arrived(q_ready, phase, a.wait_ns);
-      }
+  // Nothing that was asked for may outlive the CTA.  Where every wait was met all of it has been waited for; where one ran out, in whichever warp, copies
+  // and products get another limit each.
+  const bool late = __syncthreads_or(!ok);
+  if (warp == C::WARPS) {
+    if (late) {
+      for (int i = max(0, keys - ST); i < keys; ++i) tile_arrived(kfull + 8 * (i % ST), (i / ST) & 1, a.wait_ns);
+      for (int i = max(0, values - ST); i < values; ++i) tile_arrived(vfull + 8 * (i % ST), (i / ST) & 1, a.wait_ns);
+      if (queries) tile_arrived(q_ready, (queries - 1) & 1, a.wait_ns);
+    }
   } else if (warp == C::WARPS + 1) {
+    if (late) {
+      if (leader) umma_commit(drained);
+      __syncwarp();
+      tile_arrived(drained, 0, a.wait_ns);
+    }
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)C::COLS) : "memory");
   }

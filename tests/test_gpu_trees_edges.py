@@ -4,7 +4,7 @@ import torch
 
 from tests import trees_ref as tr
 from tests.serving_ref import Pool
-from tests.test_gpu_serving import stale
+from tests.test_gpu_serving import ints, lib, stale, stream, wide
 from tests.test_gpu_trees import BF16, check
 
 pytestmark = pytest.mark.gpu
@@ -25,3 +25,38 @@ def test_long_units_beside_short_ones(D, M, Hq):
         a = check(pool, BF16, Hq, Hkv, D, lengths, new, M, trees, window=window, sinks=sinks, seed=2)
         again = check(pool, BF16, Hq, Hkv, D, lengths, new, M, trees, window=window, sinks=sinks, seed=2, runs=10)
         assert all(torch.equal(x, y) for x, y in zip(a, again))
+
+
+@pytest.mark.parametrize("D,Hq,M", [(64, 8, 40), (128, 8, 20), (64, 16, 70)])
+@pytest.mark.parametrize("miss_from", [0, 1])
+def test_a_wait_that_runs_out_in_a_short_run(D, Hq, M, miss_from):
+    """Runs of one or two tiles: the warp that fetches has asked for all of them and meets no wait that runs out, the others do.  The call ends, says so, and
+    the next one is whole."""
+    tsfm = lib()
+    lengths = [3, 100, 128, 60]
+    pool = Pool(4, 2, D, 16, [n + M for n in lengths], BF16, seed=3)
+    q = wide((4, M), Hq * D, BF16, 0, 1)
+    pages = pool.describe(tsfm)
+    mask, depth = tr.ancestors(tr.tree("random", M, 1))
+    mask, depth = tr.words(mask).cuda(), ints(depth)
+    size = tsfm.tsfm_tree_attention_workspace(pages, 4, M, Hq, 128 + M)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+
+    def run():
+        out = torch.zeros_like(q)
+        tsfm.tsfm_tree_attention(stream(), pages, q, q.stride(1), out, out.stride(1), ints(lengths), None, mask, depth, True, 4, M, Hq, 0.125, 0, 0, 128 + M, None, ws,
+                                 size)
+        torch.cuda.synchronize()
+        return out
+
+    good = run()
+    try:
+        tsfm.tsfm_debug_tile_wait(2000, miss_from)
+        bad = run()
+    finally:
+        tsfm.tsfm_debug_tile_wait()
+    # (series 0 has one tile: nothing is missed in it from a second one on, unless its CTA has another unit's before)
+    assert miss_from or (int(pool.status) == tsfm.TSFM_PAGES_TIMEOUT and torch.isnan(bad.float()).all())
+    assert torch.isnan(bad.float()).any() == (int(pool.status) != 0)
+    pool.status.zero_()
+    assert torch.equal(run(), good) and int(pool.status) == 0
