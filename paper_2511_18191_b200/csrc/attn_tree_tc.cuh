@@ -4,18 +4,20 @@
 // A CTA takes a run of tiles as in attn_paged.cuh, of units of QT x 128 rows (new tokens x the heads of a group).  A tile is two blocks of 64 slots,
 // wherever in the cache they lie (a block with sinks beside one of the window).  Of each, for 128 rows at a time:
 //   S = Q K^T (128 x 128, queries and keys as they are: products of bf16, sums in fp32, in tensor memory); softmax by two threads a row, each
-//   the slots of one block: exponentials, sum, maximum; P back over S as bf16; O += P V in tensor memory.
+//   the slots of one block: exponentials, sum, maximum; P back over S as two bf16 parts, the high and the low ones of 16 slots in the columns that held
+//   their scores; O += P V in tensor memory, both parts.
 // Softmax is the same whatever is subtracted from the scores, as long as nothing overflows and the largest terms do not vanish.  So the exponentials
-// do not wait for the row's maximum: they are taken against a reference, 0 at first, and where the maximum turns out to lie 2^20 above it (the first
-// one: or below) the reference moves there, O is multiplied in tensor memory and the tile's exponentials are taken again.  With scores of ordinary size
-// that never happens, and O is read once, when the unit ends.  (Values above 2^100 could so overflow where a sum over 1 would not.)
+// do not wait for the row's maximum: they are taken against a reference, 0 at first, and where the maximum of the next 16 slots turns out to lie 2^20 above it (the
+// first one: or below) the reference moves there.  References are whole numbers, so what was there before follows by products with powers of two, which are exact:
+// the tile's probabilities at its end, O in tensor memory.  With scores of ordinary size that never happens, and O is read once, when the unit ends.
+// (Values above 2^100 could so overflow where a sum over 1 would not.)
 // QT = 1: two CTAs on an SM, one's products run beside the other's softmax.  QT = 2: one CTA with two times 128 rows, which share the tiles that
 // they read and take turns in the same way.
 // A slot that some row must not see never meets it as 0 x NaN: values outside the series' slots are zeroed in shared memory; in tiles that not every
 // row sees as a whole, values that are not finite are zeroed too, and rows that do see one get NaN.
-// Precision: P is rounded to bf16 once (2^-8 of a probability at most: 0.0023 of the output's norm against 64 bits, where rounding the output alone gives
-// 0.0017; a second part would add half of the tensor core's work), sums are fp32 and of the unrounded exponentials.
-// Bound: the chain of a tile's softmax (2200 cycles for 64 slots a thread, beside 1024 of products; tensor pipe 34 %, issue 0.4 a cycle).  32 series of up to 8192
+// Precision: as paged_attn_mma_kernel: 2^-16 of a probability is lost (P in two bf16 parts; with one, 2^-8, the output was off by 0.0023 of its norm where its own
+// rounding is 0.0017), sums are fp32 and of the unrounded exponentials.  The second part is half as much work again for the tensor core.
+// Bound: the chain of a tile's softmax (2200 cycles for 64 slots a thread, beside 1536 of products; tensor pipe 34 %, issue 0.4 a cycle).  32 series of up to 8192
 // slots, 61 nodes x 4 heads of 128 a key head: 199 us and 20 of the join, 520 TFLOP/s of what the definition needs, 570 MB from DRAM (87 us); 4 x 4096 tokens in a window
 // of 1024: 450 us.  What was tried and slower: half of the exponentials by FMA, the maximum in a pass of its own, values looked at by the warp of the products,
 // two groups of softmax warps on one stream of tiles.
@@ -34,7 +36,7 @@ template <int D_, int QT_> struct TreeTc {
   static constexpr int STAGES = D == 128 && QT == 1 ? 1 : 2;     // of keys and of values
   static constexpr int SMEM_BYTES = (QT + 2 * STAGES) * TILE_BYTES + 1024;       // (queries first; parts begin at multiples of 1 KB)
   static constexpr int WARPS = 8 * QT, THREADS = 32 * (WARPS + 2), CTAS = 2 / QT;
-  static constexpr int COLS = 256 * QT, O = 128 * QT;            // columns of tensor memory: scores, sums; a block's probabilities lie over its scores
+  static constexpr int COLS = 256 * QT, O = 128 * QT;            // columns of tensor memory: scores, sums; probabilities lie over their scores
   static constexpr int START = 2;                                // what starts and ends a unit, in tiles
   static_assert(CTAS * (SMEM_BYTES + 5 * 1024) <= 228 * 1024, "CTAs on an SM");
 };
@@ -330,8 +332,10 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
               if (k >= 4 && !two) break;
 #pragma unroll
               for (int p = 0; p < PARTS; ++p)
-                umma_bf16_ts(tmem + C::O + D * q + 64 * p, tmem + 128 * q + k / 4 * 64 + k % 4 * 8, dv + (uint64_t)(p * (C::PART_BYTES >> 4) + 128 * k), idesc_o,
-                             first && k == 0 ? 0u : 1u);
+#pragma unroll
+                for (int low = 0; low < 2; ++low)
+                  umma_bf16_ts(tmem + C::O + D * q + 64 * p, tmem + 128 * q + 16 * k + 8 * low, dv + (uint64_t)(p * (C::PART_BYTES >> 4) + 128 * k), idesc_o,
+                               first && k == 0 && !low ? 0u : 1u);
             }
             if (q + 1 == now) umma_commit(vempty + 8 * stage);
             umma_commit(o_full + 8 * q);
@@ -384,9 +388,13 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
         sees = here ? (part ? valid1 : valid0) & paged_tree_bits(a, span, paged_tree_range(a, span, at.b, token), at.b, token, part ? base1 : base0) : 0ull;
       }
       tc_fence_after();
-      // f(slots 16 x .. of the block, their scores), hidden ones -inf; the next ones are on their way meanwhile
-      auto each = [&](auto f) {
-        float s[2][16];
+      // The reference may move behind any 16 slots; where it did, the tile's probabilities are brought to the last one when they are all there: products
+      // with powers of two, exact in both parts.
+      float ref = m, refs[4];
+      bool any = seen, moved = false;              // the row saw something by here; its reference moved in this tile
+      uint64_t sum = 0;
+      if (here) {
+        float s[2][16];                            // 16 slots; the next ones are on their way meanwhile
         tmem_load16(mine, s[0]);
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
@@ -402,46 +410,65 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
 #pragma unroll
             for (int e = 0; e < 16; ++e) y[e] = bits >> e & 1 ? y[e] : -INFINITY;
           }
-          f(x, y);
-        }
-      };
-      uint32_t p[32];
-      float top = -INFINITY, sum = 0.f;
-      auto largest = [&](const float (&y)[16], float (&t)[2]) {
+          float t[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-        for (int e = 0; e < 16; e += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(t[e >> 1 & 1]) : "f"(y[e]), "f"(y[e + 1]));
-      };
-      auto exponentials = [&](bool with_top) {
-        const uint64_t minus = f32x2(-m, -m);
-        uint64_t sum2[2] = {0, 0};
-        float t[2] = {-INFINITY, -INFINITY};
-        each([&](int x, const float (&y)[16]) {
-          if (with_top) largest(y, t);
+          for (int e = 0; e < 16; e += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(t[e >> 1 & 1]) : "f"(y[e]), "f"(y[e + 1]));
+          const float top = fmaxf(t[0], t[1]) * scale;
+          if (top > ref + TREE_TC_SLACK || (!any && top < ref - TREE_TC_SLACK && top > -INFINITY)) {
+            const float now = ceilf(top), f = any ? flash_ex2(ref - now) : 0.f;
+            sum = mul2(sum, f32x2(f, f));
+            ref = now;
+            moved = true;
+          }
+          any |= top > -INFINITY;
+          refs[x] = ref;
+          const uint64_t minus = f32x2(-ref, -ref);
+          uint64_t here2 = 0;
+          uint32_t p[16];                          // high parts, low parts
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const float2 d = unpack2(fma2(f32x2(y[2 * e], y[2 * e + 1]), scale2, minus));
             const float p0 = flash_ex2(d.x), p1 = flash_ex2(d.y);
-            sum2[e & 1] = add2(sum2[e & 1], f32x2(p0, p1));
-            p[8 * x + e] = pack_bf16x2(p0, p1);
+            here2 = add2(here2, f32x2(p0, p1));
+            p[e] = pack_bf16x2(p0, p1);
+            const float2 low = unpack2(fma2(f32x2(__uint_as_float(p[e] << 16), __uint_as_float(p[e] & 0xffff0000u)), f32x2(-1.f, -1.f), f32x2(p0, p1)));
+            p[8 + e] = pack_bf16x2(low.x, low.y);
           }
-        });
-        const float2 both = unpack2(add2(sum2[0], sum2[1]));
-        sum = both.x + both.y;
-        if (with_top) top = fmaxf(t[0], t[1]) * scale;
-      };
-      if (here) exponentials(true);
-      // whether the row's reference moves, by one half of the tile or by both
-      auto moves = [&]() { return top > m + TREE_TC_SLACK || (!seen && top < m - TREE_TC_SLACK && top > -INFINITY); };
-      sh.top[q][part][row] = top;
-      const bool again = bar_any64(meeting, moves());
-      top = fmaxf(top, sh.top[q][part ^ 1][row]);  // (written again only after this warp's next probabilities)
-      if (again) {                                 // (both warps of these rows)
-        float alpha = 1.f;
-        if (moves()) {
-          alpha = seen ? flash_ex2(m - top) : 0.f;
-          m = top;
-          l *= alpha;
+          sum = add2(sum, here2);
+          tmem_st16(mine + 16 * x, p);
         }
+      }
+      const float2 both = unpack2(sum);
+      float mass = both.x + both.y;
+      const float own = any ? ref : -INFINITY;
+      sh.top[q][part][row] = own;
+      const bool again = bar_any64(meeting, moved);
+      const float other = sh.top[q][part ^ 1][row];        // (written again only after this warp's next probabilities)
+      if (again) {                                 // (both warps of these rows)
+        const float now = fmaxf(own, other);       // (-inf: nothing seen as yet)
+        const float alpha = seen ? flash_ex2(m - now) : 1.f;
+        // (slots before the first one that the row sees have probabilities 0 and may have a larger reference)
+        auto factor = [&](float r) { return flash_ex2(fminf(r - now, 0.f)); };
+        if (here) {
+          tmem_stored();
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const __nv_bfloat162 f = __float2bfloat162_rn(factor(refs[x]));
+            float y[16];
+            tmem_load16(mine + 16 * x, y);
+            tmem_wait16(y);
+            uint32_t w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const __nv_bfloat162 z = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&y[e]), f);
+              w[e] = *reinterpret_cast<const uint32_t *>(&z);
+            }
+            tmem_st16(mine + 16 * x, w);
+          }
+        }
+        mass *= factor(ref);
+        l *= alpha;
+        if (now > -INFINITY) m = now;
         if (!first && __any_sync(0xffffffffu, alpha != 1.f)) {
           wait(o_full + 8 * q, turn - 1);
           tc_fence_after();
@@ -456,14 +483,9 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
             tmem_st16(sums + c, r);
           }
         }
-        if (here) exponentials(false);
       }
-      seen |= top > -INFINITY;
-      if (here) {
-        l += sum;
-        tmem_st16(mine, *reinterpret_cast<uint32_t(*)[16]>(p));
-        tmem_st16(mine + 16, *reinterpret_cast<uint32_t(*)[16]>(p + 16));
-      }
+      seen = any || other > -INFINITY;
+      if (here) l += mass;
       if (!(open0 && open1)) {
         // The two threads of a row of the first 128 look at slot `row` of the tile; all warps wait for theirs, like all roles with a limit.  (The
         // second 128 rows' products follow the first's.)
