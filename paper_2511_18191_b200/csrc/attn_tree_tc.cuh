@@ -14,7 +14,7 @@
 // QT = 1: two CTAs on an SM, one's products run beside the other's softmax.  QT = 2: one CTA with two times 128 rows, which share the tiles that
 // they read and take turns in the same way.
 // A slot that some row must not see never meets it as 0 x NaN: values outside the series' slots are zeroed in shared memory; in tiles that not every
-// row sees as a whole, values that are not finite are zeroed too, and rows that do see one get NaN.
+// row sees as a whole, elements that are not finite are zeroed too, and rows that do see one get NaN in its column, and there alone.
 // Precision: as paged_attn_mma_kernel: 2^-16 of a probability is lost (P in two bf16 parts; with one, 2^-8, the output was off by 0.0023 of its norm where its own
 // rounding is 0.0017), sums are fp32 and of the unrounded exponentials.  The second part is half as much work again for the tensor core.
 // Bound: the chain of a tile's softmax (2200 cycles for 64 slots a thread, beside 1536 of products; tensor pipe 34 %, issue 0.4 a cycle).  32 series of up to 8192
@@ -38,7 +38,7 @@ template <int D_, int QT_> struct TreeTc {
   static constexpr int WARPS = 8 * QT, THREADS = 32 * (WARPS + 2), CTAS = 2 / QT;
   static constexpr int COLS = 256 * QT, O = 128 * QT;            // columns of tensor memory: scores, sums; probabilities lie over their scores
   static constexpr int START = 2;                                // what starts and ends a unit, in tiles
-  static_assert(CTAS * (SMEM_BYTES + 5 * 1024) <= 228 * 1024, "CTAs on an SM");
+  static_assert(CTAS * (SMEM_BYTES + 9 * 1024 + 512) <= 228 * 1024, "CTAs on an SM");
 };
 constexpr float TREE_TC_SLACK = 20.f;              // powers of two between a row's maximum and its reference
 
@@ -46,7 +46,8 @@ struct TreeTcShared {
   unsigned long long kfull[2], kempty[2], vfull[2], vempty[2], info[4], taken[4], s_full[2], p_ready[2], o_full[2], looked[2], q_ready, drained;
   unsigned long long valid[4][2];                  // of a tile's blocks: slots that exist
   float top[2][2][128], sum[2][2][128];            // what the two threads of a row exchange
-  uint32_t bad[4][4];                              // slots of such a tile whose values are not finite
+  uint32_t bad[4][2][4];                           // slots of such a tile with values that are not finite, in the first and the second half of the columns
+  unsigned long long columns[2][128][2];           // which, of those slots
   uint32_t tmem;
 };
 
@@ -161,7 +162,7 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
       mbar_init(info + 8 * lane, 1);
       mbar_init(taken + 8 * lane, C::WARPS);
     }
-    if (lane < 16) (&sh.bad[0][0])[lane] = 0;
+    (&sh.bad[0][0][0])[lane] = 0;
     if (lane == 0) {
       mbar_init(q_ready, 1);
       mbar_init(drained, 1);
@@ -354,7 +355,8 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
     TreeWalk at(a, run, ROWS);
     int2 open = make_int2(0, 0);
     int looks = 0, turn = 0;                       // turn: tiles of this warp's rows
-    bool from_start = false, nan_seen = false, idle = false, seen = false;       // seen: a tile held something that the row sees
+    bool from_start = false, idle = false, seen = false;       // seen: a tile held something that the row sees
+    unsigned long long spoiled = 0;                // this thread's columns in which the row sees a value that is not finite
     auto row_of = [&]() { return at.u / Hkv * ROWS + q * 128 + row; };
     float m = 0.f, l = 0.f;                        // the reference; the sum of this thread's slots
     for (int i = 0; i < run.count; ++i, at.next(a, ROWS)) {
@@ -366,7 +368,7 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
         from_start = at.t == 0;
         idle = q >= at.halves<QT>(a, span);
         open = paged_tree_open(a, span, token_of(a, row0), min(span.n_new, token_of(a, min(R, row0 + ROWS) - 1) + 1) - 1);
-        m = 0.f, l = 0.f, nan_seen = seen = false;
+        m = 0.f, l = 0.f, seen = false, spoiled = 0;
       }
       const bool two = at.two(), here = part == 0 || two;
       const int base0 = at.base(0), base1 = at.base(1);
@@ -489,37 +491,57 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
       if (!(open0 && open1)) {
         // The two threads of a row of the first 128 look at slot `row` of the tile; all warps wait for theirs, like all roles with a limit.  (The
         // second 128 rows' products follow the first's.)
-        uint32_t *const found = sh.bad[looks & 3];
         uint4 *v = reinterpret_cast<uint4 *>(smem + (values0 - smem0) + stage * C::TILE_BYTES + (PARTS == 2 ? part * C::PART_BYTES : 0) + row * 128);
-        constexpr int CH = PARTS == 2 ? 8 : 4;     // 16-byte chunks of a thread
-        const bool behind = !((row < 64 ? valid0 : valid1) >> (row & 63) & 1), open_row = row < 64 ? open0 : open1;
+        constexpr int CH = PARTS == 2 ? 8 : 4;     // 16-byte chunks of a thread: its half of the columns
+        auto chunk = [&](int x) -> uint4 & { return v[((PARTS == 2 ? x : part * 4 + x) ^ row) & 7]; };
+        uint32_t *const found = sh.bad[looks & 3][part];
         if (q == 0) {
           wait(vfull + 8 * stage, use);
-          if (!behind && !open_row) {
-            uint32_t bad = 0;                      // (an exponent of all ones carries into its sign)
+          if (!((row < 64 ? valid0 : valid1) >> (row & 63) & 1)) {
+#pragma unroll
+            for (int x = 0; x < CH; ++x) chunk(x) = make_uint4(0u, 0u, 0u, 0u);
+          } else if (!(row < 64 ? open0 : open1)) {
+            auto ones = [](uint32_t w) { return (w & 0x7f807f80u) + 0x00800080u; };      // (an exponent of all ones carries into its sign)
+            uint32_t bad = 0;
 #pragma unroll
             for (int x = 0; x < CH; ++x) {
-              const uint4 w = v[(x + (PARTS == 2 ? 0 : part * 4) + row) & 7];
-              bad |= ((w.x & 0x7f807f80u) + 0x00800080u) | ((w.y & 0x7f807f80u) + 0x00800080u) | ((w.z & 0x7f807f80u) + 0x00800080u) | ((w.w & 0x7f807f80u) + 0x00800080u);
+              const uint4 w = chunk(x);
+              bad |= ones(w.x) | ones(w.y) | ones(w.z) | ones(w.w);
             }
-            if (bad & 0x80008000u) atomicOr(found + (row >> 5), 1u << (row & 31));
+            if (bad & 0x80008000u) {
+              unsigned long long gone = 0;
+#pragma unroll 1
+              for (int x = 0; x < CH; ++x)
+#pragma unroll 1
+                for (int e = 0; e < 4; ++e) {
+                  uint32_t &w = (&chunk(x).x)[e];
+                  const uint32_t y = ones(w);
+                  gone |= (unsigned long long)((y >> 15 & 1) | (y >> 30 & 2)) << (8 * x + 2 * e);
+                  w &= (y & 0x8000u ? 0u : 0xffffu) | (y >> 31 ? 0u : 0xffff0000u);
+                }
+              sh.columns[looks & 1][row][part] = gone;
+              atomicOr(found + (row >> 5), 1u << (row & 31));
+            }
           }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) mbar_arrive(looked + 8 * (looks & 1));
         }
         wait(looked + 8 * (looks & 1), looks >> 1);
-        const unsigned long long bad = found[2 * part] | (unsigned long long)found[2 * part + 1] << 32;
-        if (q == 0) {
-          // (the one after next: who comes last is one tile behind)
-          if (tid < 4) sh.bad[(looks + 2) & 3][tid] = 0;
-          if (behind || (found[row >> 5] >> (row & 31) & 1)) {
-#pragma unroll
-            for (int x = 0; x < CH; ++x) v[(x + (PARTS == 2 ? 0 : part * 4) + row) & 7] = make_uint4(0u, 0u, 0u, 0u);
+        if (found[0] | found[1] | found[2] | found[3]) {
+          const PagedSpan span = at.span(a, ROWS);
+          const int token = row_of() < R ? token_of(a, row_of()) : a.M;
+          const int2 range = paged_tree_range(a, span, at.b, token);
+#pragma unroll 1
+          for (int x = 0; x < 2; ++x) {
+            unsigned long long bits = (found[2 * x] | (unsigned long long)found[2 * x + 1] << 32) & (x ? valid1 : valid0);
+            bits &= bits ? paged_tree_bits(a, span, range, at.b, token, x ? base1 : base0) : 0ull;
+            for (; bits; bits &= bits - 1) spoiled |= sh.columns[looks & 1][64 * x + __ffsll(bits) - 1][part];
           }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
+        // (the one after next: who comes last is one tile behind)
+        if (q == 0 && tid < 8) (&sh.bad[(looks + 2) & 3][0][0])[tid] = 0;
         ++looks;
-        nan_seen |= !all && (sees & bad) != 0;
       }
       tmem_stored();
       tc_fence_before();
@@ -528,7 +550,6 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
 
       if (at.t + 1 == at.tiles() || i + 1 == run.count) {
         // the unit, or this CTA's part of it, ends
-        if (nan_seen) l = NAN;
         sh.sum[q][part][row] = l;
         bar_any64(meeting, false);
         l = sh.sum[q][0][row] + sh.sum[q][1][row];
@@ -546,6 +567,11 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
           float o[16];
           tmem_load16(sums + c, o);
           tmem_wait16(o);
+          if (spoiled >> c & 0xffff) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (spoiled >> (c + e) & 1) o[e] = l == 0.f ? 0.f : NAN;
+          }
           if (whole) {
             if (live) {
 #pragma unroll

@@ -1,11 +1,15 @@
 """Attention of trees and windows, log probabilities: batches, masks, values and scales that the ordinary cases (tests/test_gpu_trees.py) leave out."""
+import math
+
+import numpy as np
 import pytest
 import torch
 
+from tests import serving_ref as ref
 from tests import trees_ref as tr
-from tests.serving_ref import Pool
+from tests.serving_ref import U, Pool
 from tests.test_gpu_serving import ints, lib, stale, stream, wide
-from tests.test_gpu_trees import BF16, check
+from tests.test_gpu_trees import BF16, F32, check
 
 pytestmark = pytest.mark.gpu
 
@@ -60,3 +64,54 @@ def test_a_wait_that_runs_out_in_a_short_run(D, Hq, M, miss_from):
     assert torch.isnan(bad.float()).any() == (int(pool.status) != 0)
     pool.status.zero_()
     assert torch.equal(run(), good) and int(pool.status) == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D,M,Hq", [(64, 9, 2), (32, 30, 4), (64, 26, 4), (128, 20, 8), (64, 80, 8), (128, 150, 4)])
+def test_values_that_are_not_finite_spoil_their_columns_alone(dtype, D, M, Hq):
+    """Some elements of some values are not finite, in tiles that every token sees whole and in others: log-sums and all other columns are those of a cache with 0
+    there; tokens that see the element get no number in its column, others no trace of it."""
+    tsfm = lib()
+    Hkv, lengths = 2, [300, 150, 20]
+    parent = [tr.tree("random", M, 5), tr.tree("star", M, 0), tr.tree("chain", M, 0)]
+    pool = Pool(3, Hkv, D, 16, [n + M for n in lengths], dtype, seed=3)
+    for b, n in enumerate(lengths):
+        stale(pool, b, n + M)
+    # slots: among the sinks; of windows; the last before the new tokens; some of these
+    bad = {(0, 3, 1): {0: math.nan, D - 1: math.inf}, (0, 68, 0): {5: -math.inf}, (0, 215, 1): {D // 2: math.inf}, (0, 299, 0): {D // 2 - 1: math.nan},
+           (0, 300, 1): {7: math.nan}, (0, 300 + M - 2, 0): {9: math.nan, 10: math.nan}, (1, 149, 1): {1: math.nan}, (1, 150 + M // 2, 1): {1: math.inf, 31: math.nan},
+           (2, 20, 0): {c: math.nan for c in range(D)}, (2, 25, 1): {0: -math.inf}}
+    clean = pool.v.clone()
+    for (b, s, h), columns in bad.items():
+        at = pool.table[b, s // 16].long(), h, s % 16
+        for c, x in columns.items():
+            pool.v[at][c], clean[at][c] = x, 0.0
+    q = wide((3, M), Hq * D, dtype, 0, 1, 2.0)
+    out, lse = torch.zeros_like(q), torch.zeros(3, M, Hq, device="cuda")
+    pages = pool.describe(tsfm)
+    work = torch.empty(tsfm.tsfm_tree_attention_workspace(pages, 3, M, Hq, 300 + M), dtype=torch.uint8, device="cuda")
+    for masks, window, sinks in ((None, 100, 70), ([tr.ancestors(p) for p in parent], 0, 0), ([tr.ancestors(p) for p in parent], 100, 4), (None, 0, 0)):
+        args = (stream(), pages, q, q.stride(1), out, out.stride(1), ints(lengths), None)
+        rest = (3, M, Hq, 0.125, window, sinks, 300 + M, lse, work, work.numel())
+        if masks:
+            bits, depth = torch.stack([tr.words(s) for s, _ in masks]).cuda(), ints(np.stack([d for _, d in masks]))
+            tsfm.tsfm_tree_attention(*args, bits, depth, False, *rest)
+        else:
+            tsfm.tsfm_window_attention(*args, *rest)
+        spoiled_rows = 0
+        for b, n in enumerate(lengths):
+            k, v = pool.rows(pool.k, b, n + M), pool.rows(clean, b, n + M)
+            for m in range(M):
+                seen = tr.visible(n, M, m, window, sinks, *(masks[b] if masks else (None, None)))
+                o, z, absv, peak, count = tr.attention(q[b, m].cpu().double().view(Hq, D), k, v, 0.125, seen)
+                rel = ref.attention_tolerance(dtype, D, count, peak)[:, None]
+                got = out[b, m].cpu().double().view(Hq, D)
+                spoiled = torch.zeros(Hq, D, dtype=torch.bool)
+                for (c, s, h), columns in bad.items():
+                    if c == b and seen[s]:
+                        spoiled[h * Hq // Hkv:(h + 1) * Hq // Hkv, list(columns)] = True
+                assert torch.equal(~torch.isfinite(got), spoiled), (b, m, window)
+                assert ((got - o).abs() <= U[dtype] * o.abs() + rel * absv + 1e-30)[~spoiled].all(), (b, m, window)
+                assert ((lse[b, m].cpu().double() - z).abs() <= rel[:, 0] + 4 * U[F32] * (z.abs() + peak + 1)).all(), (b, m, window)
+                spoiled_rows += int(spoiled.any())
+        assert spoiled_rows
