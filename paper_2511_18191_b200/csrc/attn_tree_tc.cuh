@@ -49,6 +49,7 @@ struct TreeTcShared {
   uint32_t bad[4][2][4];                           // slots of such a tile with values that are not finite, in the first and the second half of the columns
   unsigned long long columns[2][128][2];           // which, of those slots
   uint32_t tmem;
+  int dead;                                        // a wait ran out: what is stored from here on is NaN
 };
 
 // A CTA's way through its run; every role walks by itself.  Of the unit only what every tile asks for is kept: registers are short, and what the
@@ -166,6 +167,7 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
     if (lane == 0) {
       mbar_init(q_ready, 1);
       mbar_init(drained, 1);
+      sh.dead = 0;
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -183,6 +185,7 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
   auto wait = [&](uint32_t bar, int phase) {
     if (ok && __any_sync(0xffffffffu, !tile_arrived(bar, (uint32_t)phase & 1, a.wait_ns))) {
       ok = false;
+      sh.dead = 1;
       pages_report(a.pg, PAGES_TIMEOUT);
     }
   };
@@ -554,7 +557,8 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
         bar_any64(meeting, false);
         l = sh.sum[q][0][row] + sh.sum[q][1][row];
         wait(o_full + 8 * q, turn);
-        if (!ok) l = NAN;
+        // (a warp whose own waits were met has its rows' product from what the others left: all of them say so before the product starts)
+        if (!ok || sh.dead) l = NAN;
         tc_fence_after();
         const int r = row_of(), h = at.u % Hkv;
         const bool whole = from_start && at.t + 1 == at.tiles(), live = r < R && token_of(a, r) < at.span(a, ROWS).n_new;
