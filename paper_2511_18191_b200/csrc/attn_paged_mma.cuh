@@ -233,7 +233,8 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) paged_attn_mma_kernel(con
     // slots (rare) leave the products and are added to the rows that see them.
     unsigned long long odd = 0;
     const int from = max(mine, len_lo), to = min(mine + KEYS, total);
-    if (a.M > 1 && (C::TREE ? !open : max(from, min_end) < to || from < min(to, max_start))) {
+    // (One token of a chain sees every slot that is valid; one node's mask may hide its own.)
+    if (C::TREE ? (a.M > 1 || a.mask) && !open : a.M > 1 && (max(from, min_end) < to || from < min(to, max_start))) {
       uint32_t hit = 0;
 #pragma unroll
       for (int w = 0; w < KEYS * D / 256; ++w) {

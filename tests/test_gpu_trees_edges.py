@@ -115,3 +115,19 @@ def test_values_that_are_not_finite_spoil_their_columns_alone(dtype, D, M, Hq):
                 assert ((lse[b, m].cpu().double() - z).abs() <= rel[:, 0] + 4 * U[F32] * (z.abs() + peak + 1)).all(), (b, m, window)
                 spoiled_rows += int(spoiled.any())
         assert spoiled_rows
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D,Hq", [(32, 2), (64, 4), (128, 16), (64, 32), (32, 64)])
+@pytest.mark.parametrize("page", [16, 4])
+def test_one_node_that_does_not_see_itself(dtype, D, Hq, page):
+    """Any mask will do, one node's too: what lies in its own slot then has no influence."""
+    lengths = [0, 1, 63, 64, 200]
+    masks = [(np.zeros((1, 1), bool), np.zeros(1, np.int64))] * 5
+    for value in (math.nan, math.inf):
+        pool = Pool(5, 2, D, page, [n + 1 for n in lengths], dtype, seed=1)
+        for b, n in enumerate(lengths):
+            pool.put(pool.k, b, n, value)
+            pool.put(pool.v, b, n, value)
+        check(pool, dtype, Hq, 2, D, lengths, [1] * 5, 1, masks=masks)
+        check(pool, dtype, Hq, 2, D, lengths, [1] * 5, 1, masks=masks, window=70, sinks=3)
