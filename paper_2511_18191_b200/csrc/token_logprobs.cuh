@@ -185,7 +185,8 @@ __global__ void __launch_bounds__(LP_THREADS, LogprobShape<T>::CTAS) token_logpr
         ss[0] = m == -INFINITY ? s : s * f, tt[0] = m == -INFINITY ? t : f == 0.f ? 0.f * t : f * fmaf(s, d, t);
         ss[1] = tt[1] = 0.f;
         m = big, ref = now, from = v;
-        extreme |= big >= LP_FAR;
+        // (from 2^31 on what rounding left of ref, up to 64, could overflow as an exponent)
+        extreme |= big >= LP_FAR || fabsf(now) >= 2147483648.f;
       }
       float bs[2] = {0.f, 0.f}, bt[2] = {0.f, 0.f};        // (of the batch: shorter sums lose less)
 #pragma unroll

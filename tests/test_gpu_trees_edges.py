@@ -9,7 +9,7 @@ from tests import serving_ref as ref
 from tests import trees_ref as tr
 from tests.serving_ref import U, Pool
 from tests.test_gpu_serving import ints, lib, stale, stream, wide
-from tests.test_gpu_trees import BF16, F32, check
+from tests.test_gpu_trees import BF16, F32, check, check_logprobs
 
 pytestmark = pytest.mark.gpu
 
@@ -131,3 +131,23 @@ def test_one_node_that_does_not_see_itself(dtype, D, Hq, page):
             pool.put(pool.v, b, n, value)
         check(pool, dtype, Hq, 2, D, lengths, [1] * 5, 1, masks=masks)
         check(pool, dtype, Hq, 2, D, lengths, [1] * 5, 1, masks=masks, window=70, sinks=3)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [9, 700])
+def test_log_probabilities_of_large_logits(dtype, rows):
+    """Logits far from 0: of the whole row, as tokens' marks, in front of or behind ordinary ones."""
+    V = 6000
+    g = torch.Generator().manual_seed(4)
+    x = torch.randn(rows, V, generator=g)
+    for r, big in enumerate((-1e9, -1e10, 3e9, 1e13, -7e20, 1e28)):
+        x[r] = big * (1 + 1e-3 * x[r] if r % 2 else torch.ones(V))
+    x[6, :5000] = -1e12
+    x[7, 1000:] = -3e9
+    x[8, ::2] = -1e29
+    x = x.to(dtype).cuda()
+    tokens = torch.randint(0, V, (rows, 2), generator=g, dtype=torch.int32).cuda()
+    for scale in (1.0, 0.3, 40.0):
+        check_logprobs(x[:9], V, scale, tokens[:9].contiguous(), 5)
+    if rows > 9:
+        check_logprobs(x, V, 1.0, tokens, 3)
