@@ -151,3 +151,28 @@ def test_log_probabilities_of_large_logits(dtype, rows):
         check_logprobs(x[:9], V, scale, tokens[:9].contiguous(), 5)
     if rows > 9:
         check_logprobs(x, V, 1.0, tokens, 3)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [6, 600])
+def test_log_probabilities_at_scales_near_nothing(dtype, rows):
+    """Tokens that cannot be stay so however small the scale is, and logits up to the type's largest count as what they are."""
+    V = 3000
+    g = torch.Generator().manual_seed(2)
+    x = torch.randn(rows, V, generator=g)
+    x[0, 100:] = -math.inf
+    x[1, ::3] = -math.inf
+    x[1] *= 1e29
+    x[2] *= 1e38
+    x[3] = torch.where(torch.arange(V) % 2 == 0, 3e38, -3e38)
+    x[4, :7] = -2e30
+    x[4, 7:] = -math.inf
+    x[5] = torch.where(torch.arange(V) % 256 < 8, -9e29, -math.inf)
+    x = x.to(dtype)
+    x[torch.isinf(x) & (x > 0)] = torch.finfo(dtype).max
+    tokens = torch.randint(0, V, (rows, 2), generator=g, dtype=torch.int32).cuda()
+    x = x.cuda()
+    for scale in (1e-26, 1e-28, 1e-30, 1e-34, 1e-37, 1e-38, 1e-40, 0.25, 1e-3):
+        check_logprobs(x[:6], V, scale, tokens[:6].contiguous(), 5)
+    if rows > 6:
+        check_logprobs(x, V, 1e-30, tokens, 3)
