@@ -503,8 +503,8 @@ int tsfm_rope_append_tree(void *stream, const tsfm_rope *rope, const tsfm_kv_pag
  *   max_len  the longest series in slots, new ones included: lengths are cut to it.  It sizes the grid and the workspace, not the work
  *   workspace  256-byte aligned, tsfm_tree_attention_workspace() bytes; contents do not matter.  Calls that may overlap (two streams, two
  *            graphs) need one each
- * Head layouts, rows that see nothing, hidden slots, rows behind n_new, precision, lse and status: as tsfm_paged_attention.  With bf16 and more than 16 rows of a key
- * head (M n_heads / n_kv_heads) |v| above 2^100 may overflow.  A series' queries behind n_new may hold anything.
+ * Head layouts, rows that see nothing, hidden slots, rows behind n_new, precision, lse and status: as tsfm_paged_attention.  A series' queries behind n_new may
+ * hold anything.
  * M <= TSFM_MAX_TREE. */
 int tsfm_tree_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int64_t q_stride, void *out, int64_t out_stride,
                         const int32_t *len, const int32_t *n_new, const uint64_t *mask, const int32_t *depth, int32_t shared_tree, int32_t B,

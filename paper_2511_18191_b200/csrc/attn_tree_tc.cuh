@@ -7,10 +7,10 @@
 //   the slots of one block: exponentials, sum, maximum; P back over S as two bf16 parts, the high and the low ones of 16 slots in the columns that held
 //   their scores; O += P V in tensor memory, both parts.
 // Softmax is the same whatever is subtracted from the scores, as long as nothing overflows and the largest terms do not vanish.  So the exponentials
-// do not wait for the row's maximum: they are taken against a reference, 0 at first, and where the maximum of the next 16 slots turns out to lie 2^20 above it (the
-// first one: or below) the reference moves there.  References are whole numbers, so what was there before follows by products with powers of two, which are exact:
-// the tile's probabilities at its end, O in tensor memory.  With scores of ordinary size that never happens, and O is read once, when the unit ends.
-// (Values above 2^100 could so overflow where a sum over 1 would not.)
+// do not wait for the row's maximum: they are taken against a reference, 2^20 at first, and where the maximum of the next 16 slots turns out to lie above it (the first
+// one: or 2^40 below) the reference moves 2^20 above that.  References are whole numbers, so what was there before follows by products with powers of two, which are
+// exact: the tile's probabilities at its end, O in tensor memory.  With scores of ordinary size that never happens, and O is read once, when the unit ends.
+// No exponential is above 1, so sums overflow where those of another kernel would; what of a result lies below 2^-80 may be lost.
 // QT = 1: two CTAs on an SM, one's products run beside the other's softmax.  QT = 2: one CTA with two times 128 rows, which share the tiles that
 // they read and take turns in the same way.
 // A slot that some row must not see never meets it as 0 x NaN: values outside the series' slots are zeroed in shared memory; in tiles that not every
@@ -40,7 +40,7 @@ template <int D_, int QT_> struct TreeTc {
   static constexpr int START = 2;                                // what starts and ends a unit, in tiles
   static_assert(CTAS * (SMEM_BYTES + 9 * 1024 + 512) <= 228 * 1024, "CTAs on an SM");
 };
-constexpr float TREE_TC_SLACK = 20.f;              // powers of two between a row's maximum and its reference
+constexpr float TREE_TC_SLACK = 20.f;              // powers of two between a row's maximum and its reference when that is set; up to twice as many later
 
 struct TreeTcShared {
   unsigned long long kfull[2], kempty[2], vfull[2], vempty[2], info[4], taken[4], s_full[2], p_ready[2], o_full[2], looked[2], q_ready, drained;
@@ -361,7 +361,7 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
     bool from_start = false, idle = false, seen = false;       // seen: a tile held something that the row sees
     unsigned long long spoiled = 0;                // this thread's columns in which the row sees a value that is not finite
     auto row_of = [&]() { return at.u / Hkv * ROWS + q * 128 + row; };
-    float m = 0.f, l = 0.f;                        // the reference; the sum of this thread's slots
+    float m = TREE_TC_SLACK, l = 0.f;              // the reference; the sum of this thread's slots
     for (int i = 0; i < run.count; ++i, at.next(a, ROWS)) {
       const int stage = i % ST, use = i / ST;
       const bool first = i == 0 || at.t == 0;
@@ -371,7 +371,7 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
         from_start = at.t == 0;
         idle = q >= at.halves<QT>(a, span);
         open = paged_tree_open(a, span, token_of(a, row0), min(span.n_new, token_of(a, min(R, row0 + ROWS) - 1) + 1) - 1);
-        m = 0.f, l = 0.f, seen = false, spoiled = 0;
+        m = TREE_TC_SLACK, l = 0.f, seen = false, spoiled = 0;
       }
       const bool two = at.two(), here = part == 0 || two;
       const int base0 = at.base(0), base1 = at.base(1);
@@ -419,8 +419,8 @@ tree_attn_tc_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_consta
 #pragma unroll
           for (int e = 0; e < 16; e += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(t[e >> 1 & 1]) : "f"(y[e]), "f"(y[e + 1]));
           const float top = fmaxf(t[0], t[1]) * scale;
-          if (top > ref + TREE_TC_SLACK || (!any && top < ref - TREE_TC_SLACK && top > -INFINITY)) {
-            const float now = ceilf(top), f = any ? flash_ex2(ref - now) : 0.f;
+          if (top > ref || (!any && top < ref - 2 * TREE_TC_SLACK && top > -INFINITY)) {
+            const float now = ceilf(top) + TREE_TC_SLACK, f = any ? flash_ex2(ref - now) : 0.f;
             sum = mul2(sum, f32x2(f, f));
             ref = now;
             moved = true;

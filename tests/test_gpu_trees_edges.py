@@ -176,3 +176,33 @@ def test_log_probabilities_at_scales_near_nothing(dtype, rows):
         check_logprobs(x[:6], V, scale, tokens[:6].contiguous(), 5)
     if rows > 6:
         check_logprobs(x, V, 1e-30, tokens, 3)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,Hq", [(3, 4), (40, 4), (70, 16)])
+@pytest.mark.parametrize("score", [13.0, -13.0, 40.0])
+def test_large_values_of_many_slots(dtype, M, Hq, score):
+    """Scores that are alike, values near 2^112 (the sum of those of 8000 slots is below the largest fp32 number): their average is what comes out."""
+    tsfm = lib()
+    D, n = 64, 8000
+    pool = Pool(2, 2, D, 16, [n + M, 100 + M], dtype, fill=0.0)
+    pool.k[..., :] = 1.0
+    pool.v[..., :] = 2.0 ** 112
+    pool.v[..., 1::2] = -2.0 ** 112
+    q = torch.full((2, M, Hq * D), score / D, device="cuda").to(dtype)
+    out, lse = torch.zeros_like(q), torch.zeros(2, M, Hq, device="cuda")
+    pages = pool.describe(tsfm)
+    work = torch.empty(tsfm.tsfm_tree_attention_workspace(pages, 2, M, Hq, n + M), dtype=torch.uint8, device="cuda")
+    mask, depth = tr.ancestors(tr.tree("random", M, 1))
+    want = torch.full((D,), 2.0 ** 112, dtype=torch.float64, device="cuda")
+    want[1::2] *= -1
+    for tree in (True, False):
+        args = (stream(), pages, q, q.stride(1), out, out.stride(1), ints([n, 100]), None)
+        rest = (2, M, Hq, 1.0, 0, 0, n + M, lse, work, work.numel())
+        if tree:
+            tsfm.tsfm_tree_attention(*args, tr.words(mask).cuda(), ints(depth), True, *rest)
+        else:
+            tsfm.tsfm_window_attention(*args, *rest)
+        # equal probabilities: their sum and the values' by the same rounded terms, up to n additions either way; one rounding of the result
+        error = (out.double().view(2, M, Hq, D) / want - 1).abs().max()
+        assert error <= 2 * (n + 300) * 2.0 ** -24 + {F32: 2.0 ** -24, BF16: 2.0 ** -8}[dtype], error
