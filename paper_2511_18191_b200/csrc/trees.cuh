@@ -10,22 +10,26 @@ namespace {
 
 static_assert(TREE_MAX == TSFM_MAX_TREE && LP_MAX_TOP == TSFM_MAX_TOP, "as include/tsfm.h says");
 
-// Whether the rows of a key head go to tree_attn_tc_kernel, as far as shapes say: from 17 on.  (It takes 128 at a time, the other kernel 8, 16 or 32.  64 x 20 heads
-// of 64, 346 slots: 16 rows 54 us there, 44 in the other kernel; 17 rows 55 and 63; 33 rows 57 and 100.  16 x 8 heads of 128, 4096 slots: 16 rows 53 and
-// 51, 17 rows 54 and 78, 64 rows 61 and 132.)
-constexpr int TREE_TC_MIN_ROWS = 17;
+// Whether the rows of a key head go to tree_attn_tc_kernel, as far as shapes say: heads of 64 from 33 rows on, heads of 128 from 17.  (It takes 128 at a time, the
+// other kernel 8, 16 or 32; us there and in the other.  64 x 20 heads of 64, 346 slots: 17 rows 85 and 54, 30 rows 87 and 60, 33 rows 86 and 111.  16 x 8 heads
+// of 128, 4096 slots: 16 rows 73 and 59, 17 rows 73 and 93, 64 rows 78 and 169; 64 x 8 heads, 2048 slots, 20 rows: 136 and 181; 4 x 8 heads, 32 rows: 32 and 27.)
+constexpr int TREE_TC_MIN_ROWS_64 = 33, TREE_TC_MIN_ROWS_128 = 17;
 bool tree_on_tc(const tsfm_kv_pages *p, int M, int n_heads) {
-  return p->dtype == TSFM_BF16 && p->d_head >= 64 && p->page_size >= 8 && (long long)M * (n_heads / p->n_kv_heads) >= TREE_TC_MIN_ROWS;
+  return p->dtype == TSFM_BF16 && p->d_head >= 64 && p->page_size >= 8 &&
+         (long long)M * (n_heads / p->n_kv_heads) >= (p->d_head == 64 ? TREE_TC_MIN_ROWS_64 : TREE_TC_MIN_ROWS_128);
 }
-// Plan of either kernel; pl->bytes: what both would need (a pool's strides, which say whether TMA can read it, are not known here).
-int tree_plan(PagedPlan *pl, PagedPlan *tc, bool tree, const tsfm_kv_pages *p, int B, int M, int n_heads, int max_len) {
+// Plan of either kernel; windows: each chunk of rows has a window of its own; pl->bytes: what both would need (a pool's strides, which say whether TMA can read it, are not known here).
+int tree_plan(PagedPlan *pl, PagedPlan *tc, bool windows, const tsfm_kv_pages *p, int B, int M, int n_heads, int max_len) {
   if (int rc = paged_plan(pl, p, B, M, n_heads, max_len, false)) return rc;
   *tc = *pl;
   if (!tree_on_tc(p, M, n_heads)) return TSFM_OK;
   const long long R = (long long)M * (n_heads / p->n_kv_heads), pairs = (long long)B * p->n_kv_heads;
-  // A tree's rows all read the same slots: a CTA takes 256 of them beside one another (tree-large of 61 nodes, 4 heads a group: 220 us against 234).  A
-  // chain's chunks have each a window of their own, which more rows make longer (4096 tokens, window 1024: 499 us against 441 with 128).
-  tc->rows = tree && R > 128 ? 256 : 128;
+  // A CTA takes 256 rows beside one another, which share the slots that they read, where there are more than 128; but 257 to 384 rows are three times 128 and a
+  // unit of 256 would do half of its work for none.  (32 series of 2048 slots, 8 key heads of 128, us with 256 and with 128: 244 rows 148 and 164, 320 rows 245
+  // and 214, 400 rows 249 and 281, 640 rows 378 and 386, 1020 rows 502 and 602; a chain of these 527 and 574, one chain of 8192 tokens, 4 heads a group, 798 and
+  // 839.)  Chunks of a chain that have each a window of their own stay at 128: more rows make it longer, by a tile of its ten in prompts of any length (4 prompts
+  // of up to 4096 tokens, window 1024: 567 and 539; window 512 391 and 378; window 4096 1182 and 1254; lengths of whole blocks, window 1024: 496 and 511).
+  tc->rows = R <= 128 || windows || (R > 256 && R <= 384) ? 128 : 256;
   tc->chunks = (int)((R + tc->rows - 1) / tc->rows);
   tc->grid = (int)std::min<long long>(pairs * tc->chunks * ((max_len + 2 * PA_TILE - 1) / (2 * PA_TILE) + 1), 2 * kSms * 128 / tc->rows);
   size_t at = align256(sizeof(PagedMeta) * tc->grid);
@@ -61,7 +65,7 @@ int tree_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int6
                    int32_t window, int32_t sinks, int32_t max_len, float *lse, void *workspace, size_t workspace_bytes) {
   if (!q || !out || !len || !workspace || window < 0 || sinks < 0 || !std::isfinite(scale * kLog2E)) return TSFM_ERR_ARG;
   PagedPlan pl, tc;
-  if (int rc = tree_plan(&pl, &tc, mask != nullptr, pages, B, M, n_heads, max_len)) return rc;
+  if (int rc = tree_plan(&pl, &tc, !mask && window, pages, B, M, n_heads, max_len)) return rc;
   PagedAttnArgs a{};
   CUtensorMap k{}, v{};
   if (tree_on_tc(pages, M, n_heads)) {
@@ -112,9 +116,9 @@ int tsfm_rope_append_tree(void *stream, const tsfm_rope *rope, const tsfm_kv_pag
 }
 
 size_t tsfm_tree_attention_workspace(const tsfm_kv_pages *pages, int32_t B, int32_t M, int32_t n_heads, int32_t max_len) {
-  PagedPlan chain, tree, tc;
-  if (tree_plan(&chain, &tc, false, pages, B, M, n_heads, max_len) || tree_plan(&tree, &tc, true, pages, B, M, n_heads, max_len)) return 0;
-  return std::max(chain.bytes, tree.bytes);
+  PagedPlan pl, with_windows, tc;
+  if (tree_plan(&pl, &tc, false, pages, B, M, n_heads, max_len) || tree_plan(&with_windows, &tc, true, pages, B, M, n_heads, max_len)) return 0;
+  return std::max(pl.bytes, with_windows.bytes);
 }
 
 int tsfm_tree_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int64_t q_stride, void *out, int64_t out_stride,
