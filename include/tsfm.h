@@ -412,7 +412,7 @@ int tsfm_rope_append(void *stream, const tsfm_rope *rope, const tsfm_kv_pages *p
  * beyond rounding, and are the same each time for the same call.
  * Made for few new tokens: every 8 to 32 (fp32: 1 to 16) of a key head's M n_heads / n_kv_heads rows read all slots that any
  * token of the series sees, also where they belong to tokens m >= n_new[b].  A prompt of thousands of tokens is right but slow
- * (2048 tokens, 32 heads of 128 over 8 key heads: 0.8 ms): tsfm_window_attention, with window 0 if there is none, is made for those. */
+ * (2048 tokens, 32 heads of 128 over 8 key heads: 0.8 ms): tsfm_window_attention, with window 0 if there is none, is made for those (0.1 ms). */
 int tsfm_paged_attention(void *stream, const tsfm_kv_pages *pages, const void *q, int64_t q_stride, void *out, int64_t out_stride,
                          const int32_t *len, const int32_t *n_new, int32_t B, int32_t M, int32_t n_heads, float scale,
                          int32_t causal, int32_t window, int32_t max_len, float *lse, const float *w_in, float *w_out,
@@ -423,8 +423,8 @@ int tsfm_paged_attention(void *stream, const tsfm_kv_pages *pages, const void *q
 size_t tsfm_paged_attention_workspace(const tsfm_kv_pages *pages, int32_t B, int32_t M, int32_t n_heads, int32_t max_len,
                                       int32_t with_weights);
 
-/* Tests only, process-wide, not to be called while another thread attends: later calls of tsfm_paged_attention wait at most wait_us
- * (0, or more than the default of 100 ms: the default) for a tile of slots, and with miss_from >= 0 every CTA waits, from that
+/* Tests only, process-wide, not to be called while another thread attends: later calls of tsfm_paged_attention, tsfm_tree_attention
+ * and tsfm_window_attention wait at most wait_us (0, or more than the default of 100 ms: the default) for a tile of slots, and with miss_from >= 0 every CTA waits, from that
  * tile of its own on, for more bytes than it copies: the wait runs out, TSFM_PAGES_TIMEOUT is set, what depends on those tiles
  * is NaN, and the call ends.  Pages of less than eight slots are copied by other means and do not wait.  (0, -1) restores. */
 void tsfm_debug_tile_wait(int64_t wait_us, int32_t miss_from);

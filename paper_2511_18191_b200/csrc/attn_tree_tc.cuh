@@ -17,10 +17,11 @@
 // row sees as a whole, elements that are not finite are zeroed too, and rows that do see one get NaN in its column, and there alone.
 // Precision: as paged_attn_mma_kernel: 2^-16 of a probability is lost (P in two bf16 parts; with one, 2^-8, the output was off by 0.0023 of its norm where its own
 // rounding is 0.0017), sums are fp32 and of the unrounded exponentials.  The second part is half as much work again for the tensor core.
-// Bound: the chain of a tile's softmax (2200 cycles for 64 slots a thread, beside 1536 of products; tensor pipe 34 %, issue 0.4 a cycle).  32 series of up to 8192
-// slots, 61 nodes x 4 heads of 128 a key head: 199 us and 20 of the join, 520 TFLOP/s of what the definition needs, 570 MB from DRAM (87 us); 4 x 4096 tokens in a window
-// of 1024: 450 us.  What was tried and slower: half of the exponentials by FMA, the maximum in a pass of its own, values looked at by the warp of the products,
-// two groups of softmax warps on one stream of tiles.
+// Bound: the chain of a tile's softmax (2900 cycles for 64 slots a thread, beside 1536 of products; tensor pipe 45 %, issue 0.43 a cycle).  32 series of up to 8192
+// slots, 61 nodes x 4 heads of 128 a key head: 229 us and 20 of the join, 460 TFLOP/s of what the definition needs, 568 MB from DRAM (87 us); 4 prompts of up to 4096
+// tokens in a window of 1024: 555 us and 19.  What was tried and slower: half of the exponentials by FMA, the maximum in a pass of its own, values looked at by the
+// warp of the products, two groups of softmax warps on one stream of tiles; with two parts, 16 slots' maximum taken while those before are exponentiated (spills),
+// code of its own for tiles without masks (tree-large 225 -> 216, window-prompts 540 -> 601).
 // Warps 0 .. 8 QT - 1 softmax (row 32 (w % 4) + lane of 128, block w / 4 % 2), then one that fetches (TMA: boxes of a page, queries) and one for tensor
 // memory and products.  Every wait is bounded; when one runs out the status says so and what depends on it is NaN.
 #pragma once

@@ -133,8 +133,9 @@ __device__ __forceinline__ unsigned long long warp_sort(unsigned long long key, 
 // exponentials, the sum of d times them for the entropy, and which of its batches held its largest logit: nothing is done for the best tokens
 // while the row streams.  Behind it every thread's largest entry is one key; the n best keys' threads hold all of the n best entries (any
 // other entry lies below n of those keys), and only their columns are looked at again, from L2.
-// Bound: instructions (13 an entry and lane, 0.68 issued a cycle; the exponentials alone, 16 a cycle, take 45 us).  2048 rows of 100003 in bf16: 94 us without best
-// tokens, 111 with 10 of them, 3.7 TB/s; 1024 rows of 100000 in fp32 79 and 103.  Two vectors of bf16 a thread ahead and five CTAs on an SM: four and four took 121,
+// Bound: instructions (of a lane, executed an entry: bf16 12.2 without best tokens and 13.8 with ten, 0.73 to 0.79 issued a cycle; fp32 14.0 and 15.6; the
+// exponentials alone, 16 a cycle, take 45 us).  2048 rows of 100003 in bf16: 92 us without best tokens, 112 with 10 of them, 3.7 TB/s; 1024 rows of 100000 in fp32 75 and
+// 99.  Two vectors of bf16 a thread ahead and five CTAs on an SM: four and four took 121,
 // rows taken in turn by resident CTAs 117 to 130.
 template <typename T>
 __global__ void __launch_bounds__(LP_THREADS, LogprobShape<T>::CTAS) token_logprobs_kernel(const __grid_constant__ LogprobArgs a) {
