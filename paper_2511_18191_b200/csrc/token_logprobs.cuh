@@ -43,8 +43,8 @@ __device__ __forceinline__ float max_or_nan(float a, float b) {
   return r;
 }
 
-// (x - m) scale2.  Halves are subtracted: logits of the type's largest and lowest value are further apart than the largest float.
-__device__ __forceinline__ float base2_gap(float x, float m, float scale2) { return 2.f * ((0.5f * x - 0.5f * m) * scale2); }
+// (x - m) scale.  Halves are subtracted: logits of the type's largest and lowest value are further apart than the largest float.
+__device__ __forceinline__ float logit_gap(float x, float m, float scale) { return 2.f * ((0.5f * x - 0.5f * m) * scale); }
 
 // Reference logit m, sum of 2^d and sum of d 2^d over d = (logit - m) scale2.  (The difference comes first: logits of the type's lowest value times
 // scale2 would be -inf, and a row of nothing else is an even distribution.)
@@ -56,7 +56,7 @@ __device__ __forceinline__ LogSum log_sum_join(const LogSum &a, const LogSum &b,
   if (m == -INFINITY) return LogSum{m, a.s + b.s, a.t + b.t};            // (zeros, or NaN)
   LogSum r{m, 0.f, 0.f};
   auto add = [&](const LogSum &x) {
-    const float d = x.m == -INFINITY ? 0.f : max_or_nan(base2_gap(x.m, m, scale2), -300.f), f = x.m == -INFINITY ? 1.f : exp2f(d);
+    const float d = x.m == -INFINITY ? 0.f : max_or_nan(logit_gap(x.m, m, scale2), -300.f), f = x.m == -INFINITY ? 1.f : exp2f(d);
     r.s = fmaf(x.s, f, r.s);
     r.t += f * fmaf(x.s, d, x.t);
   };
@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(LP_THREADS, LogprobShape<T>::CTAS) token_logpr
       for (int i = 0; i < N / 2; ++i) {
         const float2 y = logits_of(r, i, T());
         float2 d = unpack2(mul2(fma2(f32x2(y.x, y.y), f32x2(0.5f, 0.5f), f32x2(ref, ref)), f32x2(a.scale2, a.scale2)));
-        d.x += d.x, d.y += d.y;                    // (halves: as base2_gap)
+        d.x += d.x, d.y += d.y;                    // (halves: as logit_gap)
         d.x = max_or_nan(d.x, -300.f), d.y = max_or_nan(d.y, -300.f);    // (2^-300 is 0, and -inf times it must be too)
         const uint64_t e = f32x2(lp_ex2(d.x), lp_ex2(d.y));
         s2 = add2(s2, e);
@@ -373,7 +373,8 @@ __global__ void __launch_bounds__(LP_THREADS, LogprobShape<T>::CTAS) token_logpr
   }
   constexpr float LN2 = 0.69314718055994530942f;
   const float log2_s = log2f(all.s);
-  auto log_prob = [&](float logit) { return all.s == 0.f ? -INFINITY : (base2_gap(logit, all.m, a.scale2) - log2_s) * LN2; };
+  // (not in base 2, in which a token at the type's lowest value would be beyond it)
+  auto log_prob = [&](float logit) { return all.s == 0.f ? -INFINITY : logit_gap(logit, all.m, a.scale) - log2_s * LN2; };
   if (tid == 0) {
     if (a.lse) a.lse[row] = all.s == 0.f ? -INFINITY : fmaf(all.m, a.scale, log2_s * LN2);
     if (a.entropy) a.entropy[row] = all.s == 0.f ? 0.f : (log2_s - all.t / all.s) * LN2;

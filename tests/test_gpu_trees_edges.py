@@ -206,3 +206,19 @@ def test_large_values_of_many_slots(dtype, M, Hq, score):
         # equal probabilities: their sum and the values' by the same rounded terms, up to n additions either way; one rounding of the result
         error = (out.double().view(2, M, Hq, D) / want - 1).abs().max()
         assert error <= 2 * (n + 300) * 2.0 ** -24 + {F32: 2.0 ** -24, BF16: 2.0 ** -8}[dtype], error
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [3, 600])
+def test_log_probabilities_of_tokens_at_the_lowest_value(dtype, rows):
+    """Finite, as their logits are."""
+    V, low = 2000, torch.finfo(dtype).min
+    x = torch.randn(rows, V, generator=torch.Generator().manual_seed(6)).to(dtype)
+    x[0, ::2] = low
+    x[1, 5:] = low
+    x[2, 7] = -2.5e38
+    tokens = torch.tensor([[4, 5, 7, 1999]] * rows, dtype=torch.int32).cuda()
+    for scale in (1.0, 0.6):
+        check_logprobs(x[:3].cuda(), V, scale, tokens[:3].contiguous(), 32)
+    if rows > 3:
+        check_logprobs(x.cuda(), V, 1.0, tokens, 2)
